@@ -22,6 +22,11 @@
  *                      so the distances can overlap the score pass.
  *   gather_kept        Sec. 3.4, Eq. 12: the kept rows X_S, in original order,
  *                      copied byte for byte for transmission.
+ *   last_rotary, last_rotary_append  rotary positions with several axes; the
+ *                      same with keys and values put into a paged cache.
+ *   last_decode_attention  attention of one new token over a paged cache.
+ *   last_cache_prune, last_cache_copy  Eq. 12 on a cache (the kept tokens
+ *                      compacted into new pages); pages copied.
  *
  * Conventions shared by every call
  *   - Pointers without a suffix are device pointers; pointers suffixed _h are
@@ -364,6 +369,191 @@ last_status last_connector(last_dtype dtype, int64_t K, int32_t Dv, int32_t Dh, 
                            float eps, const void *x, const float *gamma, const float *beta,
                            const void *w1, const float *b1, const void *w2, const float *b2,
                            void *out, void *ws, size_t ws_bytes, void *stream);
+
+/*
+ * The paged cache of keys and values that answers are decoded from (Sec. 3.2,
+ * 3.4: the cloud model reads the transmitted tokens, then produces its answer
+ * token by token). G layers, each n_pages pages of page_size tokens:
+ *   element (layer l, page p, head h, token t, d) of k lies at
+ *   k[l layer_stride + p page_stride + h head_stride + t token_stride + d],
+ *   strides in elements; v has the same layout.
+ * Any order of layer, page, head and token is accepted as long as no two rows
+ * of Dh elements overlap (the strides nest) and every row is 16-byte aligned.
+ * page_size is a power of two in [8, 1024] and Dh 64 or 128 (others:
+ * LAST_ERR_UNSUPPORTED). k and v must not overlap each other.
+ */
+typedef struct last_cache {
+  int32_t G, n_pages, page_size, Hkv, Dh;
+  last_dtype dtype;
+  int64_t layer_stride, page_stride, head_stride, token_stride;
+  void *k, *v;
+} last_cache;
+
+/*
+ * The sequences of a cache.
+ *   R          sequences (>= 1)
+ *   max_pages  entries of a page table row; max_pages * page_size <= 2^30
+ *              (LAST_ERR_UNSUPPORTED otherwise)
+ *   table      [R][max_pages] device: token t of sequence r lies in page
+ *              table[r][t / page_size], the same page in every layer. Entries
+ *              behind a sequence's last page are never read.
+ *   table_h    host copy, or NULL where the call allows it
+ *   lens       [R] device: tokens of each sequence, 0 allowed
+ *   lens_h     [R] host: what lens holds, or (calls that say so) a bound of it
+ * The page table and the lengths may change between the replays of a captured
+ * call, so the kernels check them too: a page outside [0, n_pages) or a
+ * length outside its bound is never followed.
+ */
+typedef struct last_pages {
+  int32_t R, max_pages;
+  const int32_t *table, *table_h;
+  const int32_t *lens, *lens_h;
+} last_pages;
+
+/*
+ * A rotation of heads by positions with one to four axes (for visual tokens
+ * time, height and width; for text all axes hold the same position):
+ *   a_i = pos[axis[i]] * inv_freq[i],  i = 0 .. n_freqs - 1
+ *   (x, y) -> (x cos a_i - y sin a_i, y cos a_i + x sin a_i)
+ * for the pairs (x, y) = elements (i, i + n_freqs) of a head, or (2i, 2i + 1)
+ * with adjacent != 0. Elements from 2 n_freqs on pass unchanged. inverse != 0
+ * turns by -a_i: the inverse, which is also the gradient (the rotation is
+ * orthogonal: dx = R^T dy).
+ *   inv_freq   [n_freqs] device fp32, taken as they are: the angle is their
+ *              product with the position in 64 bits
+ *   axis       [n_freqs] device, and axis_h its host copy: each in [0, n_axes)
+ * n_freqs is a positive multiple of 8 with 2 n_freqs <= Dh (others:
+ * LAST_ERR_UNSUPPORTED), 1 <= n_axes <= 4.
+ */
+typedef struct last_rotation {
+  int32_t n_axes, n_freqs, adjacent, inverse;
+  const float *inv_freq;
+  const int32_t *axis, *axis_h;
+} last_rotation;
+
+/*
+ * Rows of heads, [G][T][heads][Dh]: element (g, t, h, d) lies at
+ * data[g layer_stride + t token_stride + h Dh + d] (strides in elements), so
+ * that q, k and v may be parts of one projection's output. Rows are 16-byte
+ * aligned. What is only read may repeat (stride 0); what is written may not.
+ */
+typedef struct last_heads {
+  void *data;
+  int64_t layer_stride, token_stride;
+} last_heads;
+
+/*
+ * The rotary embedding that last_prefill_attention and the score calls expect
+ * their q and k to carry: q_out = rot(q), k_out = rot(k).
+ *   G, T       layers and tokens (T >= 0); every layer has the same positions
+ *   Hq, Hkv    heads of q and k; one of them may be 0, its rows are then not
+ *              read and may be NULL
+ *   Dh         64 or 128 (others: LAST_ERR_UNSUPPORTED)
+ *   dtype      of all rows (LAST_F32 or LAST_BF16); turned in fp32, rounded
+ *              once, to nearest even
+ *   pos        [n_axes][T] int32 positions, any value
+ * In place (q_out the same rows as q, k_out as k) is allowed; other overlaps
+ * of what is written with what is read are not.
+ */
+last_status last_rotary(const last_rotation *rot, last_dtype dtype, int32_t G, int32_t T,
+                        int32_t Hq, int32_t Hkv, int32_t Dh, const int32_t *pos,
+                        const last_heads *q, const last_heads *k, const last_heads *q_out,
+                        const last_heads *k_out, void *stream);
+
+/*
+ * last_rotary with the turned keys, and the values, written into a cache:
+ * the new tokens of sequence r become its last ones, at positions
+ * lens[r] - n_r .. lens[r] - 1 of the sequence, where n_r is their number. So
+ * lens counts them already, and the same last_pages serve the decoding step
+ * that follows.
+ *   rot        NULL: nothing is turned (keys are stored as they are, q and
+ *              pos are not read, and Hq must be 0)
+ *   c          the cache; layers [layer, layer + G) are written, row g of k
+ *              and v into layer + g
+ *   p          sequences; lens_h bounds lens from above, table_h may be NULL
+ *   T          new tokens of all sequences
+ *   cu_new     [R+1] CSR offsets of each sequence's new tokens, which end at
+ *              T (device and host copy); both NULL: one token per sequence, T = R
+ *   pos        [n_axes][T] positions of the rotation (not of the cache)
+ *   q, q_out   [G][T][Hq][Dh]; Hq may be 0 (not read then)
+ *   k, v       [G][T][Hkv][Dh], the cache's dtype; not part of the cache
+ * A token whose place lies before the sequence's start, behind the bound
+ * max(lens_h), or in a page outside the cache is not stored (its q_out is
+ * still written): a padded batch gives its empty slots lens[r] = 0.
+ * No two sequences may write the same page.
+ */
+last_status last_rotary_append(const last_rotation *rot, const last_cache *c, int32_t layer,
+                               int32_t G, const last_pages *p, int32_t T, const int32_t *cu_new,
+                               const int32_t *cu_new_h, int32_t Hq, const int32_t *pos,
+                               const last_heads *q, const last_heads *q_out, const last_heads *k,
+                               const last_heads *v, void *stream);
+
+/* Workspace bytes last_decode_attention needs: a function of lens_h, which
+ * need not be exact (0 if the arguments are invalid, at least 256 otherwise). */
+size_t last_decode_attention_workspace(const last_cache *c, const last_pages *p, int32_t Hq);
+
+/*
+ * Attention of one new token per sequence over its cached keys and values,
+ * the decoding counterpart of last_prefill_attention:
+ *   s_j = sigma q_r . k_j,  j = 0 .. lens[r] - 1
+ *   out_r = sum_j e^(s_j - lse) v_j,  lse = ln sum_j e^(s_j)
+ * per query head; query head h reads KV head h / (Hq / Hkv). A sequence of
+ * length 0 gives out 0 and lse -inf; one whose page table names a page outside
+ * the cache (within its length) gives NaN in both.
+ *   layer      the layer read
+ *   p          lens_h bounds lens from above (it shapes the launch; a captured
+ *              call may be replayed with any lens within it); table_h may be NULL
+ *   Hq         query heads, a multiple of the cache's Hkv
+ *   scale      sigma; <= 0 selects 1/sqrt(Dh)
+ *   q          [R][Hq][Dh] after the rotary embedding, row r at r * q_stride
+ *              elements, 16-byte aligned
+ *   out        [R][Hq][Dh] out, the cache's dtype, rounded to nearest even
+ *   lse        optional [R][Hq] fp32 out (NULL to skip)
+ *   ws         last_decode_attention_workspace bytes, 256-byte aligned; calls
+ *              that may overlap in time need their own
+ * Logits, softmax statistics, probabilities and sums are held in fp32 (for
+ * bf16 caches a probability enters the value product as the sum of two bf16
+ * numbers, within 2^-16 of it; an infinite value may so give NaN instead of
+ * infinity). A long cache is split over blocks whose
+ * partial results are joined in a fixed order.
+ */
+last_status last_decode_attention(const last_cache *c, int32_t layer, const last_pages *p,
+                                  int32_t Hq, float scale, const void *q, int64_t q_stride,
+                                  void *out, float *lse, void *ws, size_t ws_bytes, void *stream);
+
+/*
+ * Sec. 3.4, Eq. 12 on a cache: after the selection, a prompt's cache keeps its
+ * text and the kept visual tokens only, in their order, in every layer:
+ *   new token i comes from token  i                          i < vis_start
+ *                                 vis_start + kept[i - vis_start]   the K_r next
+ *                                 i - K_r + N_r              the rest
+ *   src        the sequences as they are; lens_h exact, table_h required;
+ *              vis_start + N_r <= lens
+ *   dst        where they go, R and max_pages of its own, table_h required;
+ *              lens_h[r] >= the new length lens - N_r + K_r; lens is not read
+ *   vis_start, cu_vis  the visual spans as in last_batch (N_r >= 0)
+ *   kept, cu_keep      as from diverse_select (0 <= K_r <= N_r): an index
+ *              outside [0, N_r) yields a zero-filled row
+ *   new_lens   optional [R] device out: the new lengths; not src->lens
+ * Pages that dst writes must be listed once and not by src (LAST_ERR_INVALID):
+ * the source stays whole, so other sequences may share its pages. The
+ * exception is a page wholly before vis_start that both tables name at the
+ * same place: it is shared and not copied.
+ */
+last_status last_cache_prune(const last_cache *c, const last_pages *src, const last_pages *dst,
+                             const int32_t *vis_start, const int32_t *vis_start_h,
+                             const int32_t *cu_vis, const int32_t *cu_vis_h, const int32_t *kept,
+                             const int32_t *cu_keep, const int32_t *cu_keep_h, int32_t *new_lens,
+                             void *stream);
+
+/*
+ * Copies n pages, keys and values of every layer, byte for byte: page src[i]
+ * to page dst[i] (a forked sequence's last, partly filled page; pages moved
+ * together). No page may be a target twice, or both source and target
+ * (LAST_ERR_INVALID). src and dst: [n] device arrays with host copies, n >= 0.
+ */
+last_status last_cache_copy(const last_cache *c, int32_t n, const int32_t *src, const int32_t *src_h,
+                            const int32_t *dst, const int32_t *dst_h, void *stream);
 
 /* Sec. 3.2, Eq. 2: K = ceil(N * rho_num / rho_den), integer-exact, clamped
  * to [1, N]; returns -1 for N < 1 or a ratio outside (0, 1]. */

@@ -1,8 +1,9 @@
 // C ABI of liblast: argument validation on the host, workspace sizing, and the
-// launch sequences of the three calls declared in include/last.h. Also the
+// launch sequences of the calls declared in include/last.h. Also the
 // status strings and the optional per-kernel event timing.
 #include <math.h>
 #include <stdio.h>
+#include <stdlib.h>
 #include <string.h>
 
 #include <algorithm>
@@ -546,6 +547,334 @@ last_status last_connector(last_dtype dtype, int64_t K, int32_t Dv, int32_t Dh, 
   const hipError_t e = launch_connector(K, Dv, Dh, Do, eps, x, gamma, beta, w1, b1, w2, b2, out, xn, hid,
                                         (hipStream_t)stream);
   return e == hipSuccess ? LAST_OK : LAST_ERR_DEVICE;
+}
+
+}  // extern "C"
+
+// ------------------------------------------------------------ paged cache
+namespace last {
+
+constexpr int64_t kMaxStride = (int64_t)1 << 48;
+constexpr int64_t kMaxBlocks = (int64_t)1 << 24;   // 256 threads each: a launch holds under 2^32
+
+static int64_t piece_elems(last_dtype dt) { return dt == LAST_BF16 ? 8 : 4; }
+static int32_t log2_of(int32_t x) { return 31 - __builtin_clz((unsigned)x); }
+
+static last_status check_cache(const last_cache *c) {
+  if (!c || c->G < 1 || c->n_pages < 1 || c->page_size < 1 || c->Hkv < 1 || c->Dh < 1) return LAST_ERR_INVALID;
+  if (c->dtype != LAST_F32 && c->dtype != LAST_BF16) return LAST_ERR_INVALID;
+  if (c->page_size < 8 || c->page_size > 1024 || (c->page_size & (c->page_size - 1))) return LAST_ERR_UNSUPPORTED;
+  if ((c->Dh != 64 && c->Dh != 128) || c->Hkv > 65536) return LAST_ERR_UNSUPPORTED;
+  // no two rows may overlap: sorted by stride, each index spans what lies inside it
+  struct Dim {
+    int64_t stride, size;
+  } d[4] = {{c->layer_stride, c->G}, {c->page_stride, c->n_pages}, {c->head_stride, c->Hkv},
+            {c->token_stride, c->page_size}};
+  for (const Dim &x : d)
+    if (x.size > 1 && (x.stride < c->Dh || x.stride > kMaxStride || x.stride % piece_elems(c->dtype)))
+      return LAST_ERR_INVALID;
+  std::sort(d, d + 4, [](const Dim &a, const Dim &b) { return a.stride < b.stride; });
+  int64_t span = c->Dh;
+  for (const Dim &x : d) {
+    if (x.size == 1) continue;
+    if (x.stride < span || x.size > kMaxStride / x.stride) return LAST_ERR_INVALID;
+    span += x.stride * (x.size - 1);
+  }
+  if (!c->k || !c->v || c->k == c->v || !aligned(c->k, 16) || !aligned(c->v, 16)) return LAST_ERR_INVALID;
+  return LAST_OK;
+}
+
+static last_status check_pages(const last_cache *c, const last_pages *p, bool need_table) {
+  if (!p || p->R < 1 || p->max_pages < 1 || !p->table || !p->lens_h) return LAST_ERR_INVALID;
+  if (need_table && !p->table_h) return LAST_ERR_INVALID;
+  const int64_t room = (int64_t)p->max_pages * c->page_size;
+  if (room > (int64_t)1 << 30) return LAST_ERR_UNSUPPORTED;
+  for (int32_t r = 0; r < p->R; ++r)
+    if (p->lens_h[r] < 0 || p->lens_h[r] > room) return LAST_ERR_INVALID;
+  if (p->table_h) {
+    uint32_t bad = 0;
+    for (int32_t r = 0; r < p->R; ++r) {
+      const int32_t *row = p->table_h + (int64_t)r * p->max_pages;
+      const int32_t n = (int32_t)(((int64_t)p->lens_h[r] + c->page_size - 1) / c->page_size);
+      for (int32_t i = 0; i < n; ++i) bad |= (uint32_t)((uint32_t)row[i] >= (uint32_t)c->n_pages);
+    }
+    if (bad) return LAST_ERR_INVALID;
+  }
+  return LAST_OK;
+}
+
+static last_status check_rotation(const last_rotation *rot, int32_t Dh) {
+  if (rot->n_axes < 1 || rot->n_freqs < 1 || 2 * (int64_t)rot->n_freqs > Dh) return LAST_ERR_INVALID;
+  if (!rot->inv_freq || !rot->axis || !rot->axis_h || !aligned(rot->inv_freq, 4)) return LAST_ERR_INVALID;
+  if (rot->n_axes > 4 || rot->n_freqs % 8) return LAST_ERR_UNSUPPORTED;
+  for (int32_t i = 0; i < rot->n_freqs; ++i)
+    if (rot->axis_h[i] < 0 || rot->axis_h[i] >= rot->n_axes) return LAST_ERR_INVALID;
+  return LAST_OK;
+}
+
+// Rows [G][T][H][Dh]: aligned, strides not negative, and no two rows written
+// on top of each other.
+static bool heads_ok(const last_heads *x, int32_t G, int32_t T, int32_t H, int32_t Dh, last_dtype dt, bool written) {
+  if (!x || !x->data || !aligned(x->data, 16)) return false;
+  const int64_t ts = x->token_stride, ls = x->layer_stride, row = (int64_t)H * Dh, v = piece_elems(dt);
+  if (ts < 0 || ls < 0 || ts > kMaxStride || ls > kMaxStride) return false;
+  if ((T > 1 && (ts % v || ts > kMaxStride / T)) || (G > 1 && (ls % v || ls > kMaxStride / G))) return false;
+  if (!written) return true;
+  if (T > 1 && ts < row) return false;
+  // layers behind each other, or tokens behind each other with the layers inside
+  const int64_t layer = T > 1 ? ts * (T - 1) + row : row;
+  return G <= 1 || ls >= layer || (ls >= row && (T <= 1 || ts >= ls * (G - 1) + row));
+}
+
+static void rotation_args(RotaryArgs *a, const last_rotation *rot) {
+  a->inv_freq = rot->inv_freq;
+  a->axis = rot->axis;
+  a->F = rot->n_freqs;
+  a->adjacent = rot->adjacent != 0;
+  a->inverse = rot->inverse != 0;
+}
+
+// Pages seen so far, a bit each. False from ok() where there is no memory.
+struct PageSet {
+  uint64_t *bits;
+  explicit PageSet(int32_t n) : bits(static_cast<uint64_t *>(calloc(((size_t)n + 63) / 64, 8))) {}
+  ~PageSet() { free(bits); }
+  PageSet(const PageSet &) = delete;
+  PageSet &operator=(const PageSet &) = delete;
+  bool ok() const { return bits != nullptr; }
+  bool has(int32_t p) const { return bits[p >> 6] >> (p & 63) & 1; }
+  void add(int32_t p) { bits[p >> 6] |= (uint64_t)1 << (p & 63); }
+};
+
+}  // namespace last
+
+extern "C" {
+
+last_status last_rotary(const last_rotation *rot, last_dtype dtype, int32_t G, int32_t T, int32_t Hq,
+                        int32_t Hkv, int32_t Dh, const int32_t *pos, const last_heads *q,
+                        const last_heads *k, const last_heads *q_out, const last_heads *k_out,
+                        void *stream) {
+  if (!rot || G < 1 || T < 0 || Hq < 0 || Hkv < 0 || (Hq == 0 && Hkv == 0)) return LAST_ERR_INVALID;
+  if (dtype != LAST_F32 && dtype != LAST_BF16) return LAST_ERR_INVALID;
+  if (Dh < 1) return LAST_ERR_INVALID;
+  if ((Dh != 64 && Dh != 128) || Hq > 65536 || Hkv > 65536) return LAST_ERR_UNSUPPORTED;
+  const last_status st = check_rotation(rot, Dh);
+  if (st != LAST_OK) return st;
+  if (T == 0) return LAST_OK;
+  if (!pos) return LAST_ERR_INVALID;
+  if (Hq && (!heads_ok(q, G, T, Hq, Dh, dtype, false) || !heads_ok(q_out, G, T, Hq, Dh, dtype, true)))
+    return LAST_ERR_INVALID;
+  if (Hkv && (!heads_ok(k, G, T, Hkv, Dh, dtype, false) || !heads_ok(k_out, G, T, Hkv, Dh, dtype, true)))
+    return LAST_ERR_INVALID;
+  RotaryArgs a{};
+  rotation_args(&a, rot);
+  a.pos = pos;
+  a.G = G, a.T = T, a.Hq = Hq, a.Hkv = Hkv;
+  if (Hq) {
+    a.q = q->data, a.q_ls = q->layer_stride, a.q_ts = q->token_stride;
+    a.q_out = q_out->data, a.qo_ls = q_out->layer_stride, a.qo_ts = q_out->token_stride;
+    if (q->data == q_out->data && ((T > 1 && a.q_ts != a.qo_ts) || (G > 1 && a.q_ls != a.qo_ls)))
+      return LAST_ERR_INVALID;
+  }
+  if (Hkv) {
+    a.k = k->data, a.k_ls = k->layer_stride, a.k_ts = k->token_stride;
+    a.k_out = k_out->data, a.ko_ls = k_out->layer_stride, a.ko_ts = k_out->token_stride;
+    if (k->data == k_out->data && ((T > 1 && a.k_ts != a.ko_ts) || (G > 1 && a.k_ls != a.ko_ls)))
+      return LAST_ERR_INVALID;
+  }
+  if (rotary_blocks(a, false) >= kMaxBlocks) return LAST_ERR_UNSUPPORTED;
+  return launch_rotary(a, dtype, Dh, false, (hipStream_t)stream) == hipSuccess ? LAST_OK : LAST_ERR_DEVICE;
+}
+
+last_status last_rotary_append(const last_rotation *rot, const last_cache *c, int32_t layer, int32_t G,
+                               const last_pages *p, int32_t T, const int32_t *cu_new,
+                               const int32_t *cu_new_h, int32_t Hq, const int32_t *pos,
+                               const last_heads *q, const last_heads *q_out, const last_heads *k,
+                               const last_heads *v, void *stream) {
+  last_status st = check_cache(c);
+  if (st != LAST_OK) return st;
+  if ((st = check_pages(c, p, false)) != LAST_OK) return st;
+  if (!p->lens || layer < 0 || G < 1 || G > c->G - layer || T < 0 || Hq < 0) return LAST_ERR_INVALID;
+  if (Hq > 65536) return LAST_ERR_UNSUPPORTED;
+  if (rot && (st = check_rotation(rot, c->Dh)) != LAST_OK) return st;
+  if (!rot && Hq) return LAST_ERR_INVALID;
+  if (!cu_new != !cu_new_h) return LAST_ERR_INVALID;
+  bool single = T == p->R;   // one token each
+  if (cu_new_h) {
+    if (!csr_ok(cu_new_h, p->R, 0) || cu_new_h[p->R] != T) return LAST_ERR_INVALID;
+    for (int32_t r = 0; r < p->R; ++r) single = single && cu_new_h[r + 1] - cu_new_h[r] == 1;
+  } else if (!single) {
+    return LAST_ERR_INVALID;
+  }
+  if (T == 0) return LAST_OK;
+  if ((rot && !pos) || !heads_ok(k, G, T, c->Hkv, c->Dh, c->dtype, false) ||
+      !heads_ok(v, G, T, c->Hkv, c->Dh, c->dtype, false))
+    return LAST_ERR_INVALID;
+  if (Hq && (!heads_ok(q, G, T, Hq, c->Dh, c->dtype, false) || !heads_ok(q_out, G, T, Hq, c->Dh, c->dtype, true)))
+    return LAST_ERR_INVALID;
+  RotaryArgs a{};
+  if (rot) rotation_args(&a, rot);
+  a.pos = pos;
+  a.G = G, a.T = T, a.Hq = Hq, a.Hkv = c->Hkv;
+  if (Hq) {
+    a.q = q->data, a.q_ls = q->layer_stride, a.q_ts = q->token_stride;
+    a.q_out = q_out->data, a.qo_ls = q_out->layer_stride, a.qo_ts = q_out->token_stride;
+    if (q->data == q_out->data && ((T > 1 && a.q_ts != a.qo_ts) || (G > 1 && a.q_ls != a.qo_ls)))
+      return LAST_ERR_INVALID;
+  }
+  a.k = k->data, a.k_ls = k->layer_stride, a.k_ts = k->token_stride;
+  a.v = v->data, a.v_ls = v->layer_stride, a.v_ts = v->token_stride;
+  const size_t e = c->dtype == LAST_BF16 ? 2 : 4;
+  a.k_out = static_cast<char *>(c->k) + (size_t)(c->G > 1 ? layer * c->layer_stride : 0) * e;
+  a.v_out = static_cast<char *>(c->v) + (size_t)(c->G > 1 ? layer * c->layer_stride : 0) * e;
+  a.ko_ls = c->layer_stride;
+  a.table = p->table, a.lens = p->lens, a.cu_new = single ? nullptr : cu_new;
+  a.R = p->R, a.max_pages = p->max_pages, a.n_pages = c->n_pages, a.lg_page = log2_of(c->page_size);
+  for (int32_t r = 0; r < p->R; ++r) a.max_len = std::max(a.max_len, p->lens_h[r]);
+  a.page_stride = c->page_stride, a.head_stride = c->head_stride, a.slot_stride = c->token_stride;
+  if (rotary_blocks(a, true) >= kMaxBlocks) return LAST_ERR_UNSUPPORTED;
+  return launch_rotary(a, c->dtype, c->Dh, true, (hipStream_t)stream) == hipSuccess ? LAST_OK : LAST_ERR_DEVICE;
+}
+
+static last_status check_decode(const last_cache *c, const last_pages *p, int32_t Hq, DecodePlan *d) {
+  last_status st = check_cache(c);
+  if (st != LAST_OK) return st;
+  if ((st = check_pages(c, p, false)) != LAST_OK) return st;
+  if (Hq < 1 || Hq % c->Hkv) return LAST_ERR_INVALID;
+  *d = make_decode_plan(c, p, Hq);
+  if (d->blocks >= kMaxBlocks || (int64_t)p->R * Hq >= kMaxBlocks) return LAST_ERR_UNSUPPORTED;
+  return LAST_OK;
+}
+
+static size_t decode_ws(const last_cache *c, const last_pages *p, int32_t Hq, const DecodePlan &d, void *ws,
+                        float **part_o, float2 **part_ml) {
+  Carver cv(ws);
+  const size_t rows = d.parts > 1 ? (size_t)p->R * Hq * d.parts : 0;
+  float *o = cv.take<float>(rows * c->Dh);
+  float2 *ml = cv.take<float2>(rows);
+  if (part_o) *part_o = o;
+  if (part_ml) *part_ml = ml;
+  return std::max<size_t>(256, cv.size());
+}
+
+size_t last_decode_attention_workspace(const last_cache *c, const last_pages *p, int32_t Hq) {
+  DecodePlan d;
+  if (check_decode(c, p, Hq, &d) != LAST_OK) return 0;
+  return decode_ws(c, p, Hq, d, nullptr, nullptr, nullptr);
+}
+
+last_status last_decode_attention(const last_cache *c, int32_t layer, const last_pages *p, int32_t Hq,
+                                  float scale, const void *q, int64_t q_stride, void *out, float *lse,
+                                  void *ws, size_t ws_bytes, void *stream) {
+  DecodePlan d;
+  const last_status st = check_decode(c, p, Hq, &d);
+  if (st != LAST_OK) return st;
+  if (!p->lens || layer < 0 || layer >= c->G || !std::isfinite(scale)) return LAST_ERR_INVALID;
+  if (!q || !out || !aligned(q, 16) || !aligned(out, 16) || (lse && !aligned(lse, 4))) return LAST_ERR_INVALID;
+  if (p->R > 1 && (q_stride < 0 || q_stride > kMaxStride / p->R || q_stride % piece_elems(c->dtype)))
+    return LAST_ERR_INVALID;
+  DecodeArgs a{};
+  const size_t need = decode_ws(c, p, Hq, d, nullptr, nullptr, nullptr);
+  if (!ws || ws_bytes < need || !aligned(ws, 256)) return LAST_ERR_WORKSPACE;
+  decode_ws(c, p, Hq, d, ws, &a.part_o, &a.part_ml);
+  const size_t e = c->dtype == LAST_BF16 ? 2 : 4, at = (size_t)(c->G > 1 ? layer * c->layer_stride : 0) * e;
+  a.k = static_cast<const char *>(c->k) + at;
+  a.v = static_cast<const char *>(c->v) + at;
+  a.q = q, a.out = out, a.lse = lse;
+  a.table = p->table, a.lens = p->lens;
+  a.page_stride = c->page_stride, a.head_stride = c->head_stride, a.token_stride = c->token_stride;
+  a.q_stride = p->R > 1 ? q_stride : 0;
+  a.R = p->R, a.Hq = Hq, a.Hkv = c->Hkv, a.group = Hq / c->Hkv;
+  a.max_pages = p->max_pages, a.n_pages = c->n_pages, a.lg_page = log2_of(c->page_size);
+  a.keys = d.keys, a.parts = d.parts, a.head_tiles = d.head_tiles, a.max_len = d.max_len;
+  a.scale_log2 = (scale > 0.f ? scale : 1.0f / sqrtf((float)c->Dh)) * 1.4426950408889634f;
+  return launch_decode(a, c->dtype, c->Dh, (hipStream_t)stream) == hipSuccess ? LAST_OK : LAST_ERR_DEVICE;
+}
+
+last_status last_cache_prune(const last_cache *c, const last_pages *src, const last_pages *dst,
+                             const int32_t *vis_start, const int32_t *vis_start_h, const int32_t *cu_vis,
+                             const int32_t *cu_vis_h, const int32_t *kept, const int32_t *cu_keep,
+                             const int32_t *cu_keep_h, int32_t *new_lens, void *stream) {
+  last_status st = check_cache(c);
+  if (st != LAST_OK) return st;
+  if ((st = check_pages(c, src, true)) != LAST_OK) return st;
+  if ((st = check_pages(c, dst, true)) != LAST_OK) return st;
+  const int32_t R = src->R, ps = c->page_size;
+  if (dst->R != R || !src->lens || !vis_start || !cu_vis || !cu_keep || !vis_start_h) return LAST_ERR_INVALID;
+  if (!csr_ok(cu_vis_h, R, 0) || !csr_ok(cu_keep_h, R, 0)) return LAST_ERR_INVALID;
+  if ((cu_keep_h[R] > 0 && !kept) || (new_lens && new_lens == src->lens)) return LAST_ERR_INVALID;
+  PruneArgs a{};
+  for (int32_t r = 0; r < R; ++r) {
+    const int32_t n = cu_vis_h[r + 1] - cu_vis_h[r], k = cu_keep_h[r + 1] - cu_keep_h[r], len = src->lens_h[r];
+    if (k > n || vis_start_h[r] < 0 || (int64_t)vis_start_h[r] + n > len || dst->lens_h[r] < len - n + k)
+      return LAST_ERR_INVALID;
+    a.max_old = std::max(a.max_old, len);
+    a.max_new = std::max(a.max_new, len - n + k);
+  }
+  {   // no page written may be read, or be written twice
+    PageSet read(c->n_pages), written(c->n_pages);
+    if (!read.ok() || !written.ok()) return LAST_ERR_UNSUPPORTED;
+    for (int32_t r = 0; r < R; ++r)
+      for (int32_t i = 0; i < (src->lens_h[r] + ps - 1) / ps; ++i)
+        read.add(src->table_h[(int64_t)r * src->max_pages + i]);
+    for (int32_t r = 0; r < R; ++r) {
+      const int32_t m = src->lens_h[r] - (cu_vis_h[r + 1] - cu_vis_h[r]) + (cu_keep_h[r + 1] - cu_keep_h[r]);
+      for (int32_t i = 0; i < (m + ps - 1) / ps; ++i) {
+        const int32_t to = dst->table_h[(int64_t)r * dst->max_pages + i];
+        if ((int64_t)(i + 1) * ps <= vis_start_h[r] && to == src->table_h[(int64_t)r * src->max_pages + i]) continue;
+        if (read.has(to) || written.has(to)) return LAST_ERR_INVALID;
+        written.add(to);
+      }
+    }
+  }
+  const int64_t v = piece_elems(c->dtype);
+  a.k = c->k, a.v = c->v;
+  a.src = src->table, a.dst = dst->table, a.lens = src->lens;
+  a.vis_start = vis_start, a.cu_vis = cu_vis, a.kept = kept, a.cu_keep = cu_keep, a.new_lens = new_lens;
+  a.layer_stride = c->layer_stride / v, a.page_stride = c->page_stride / v;
+  a.head_stride = c->head_stride / v, a.token_stride = c->token_stride / v;
+  a.R = R, a.G = c->G, a.Hkv = c->Hkv, a.n_pages = c->n_pages;
+  a.src_pages = src->max_pages, a.dst_pages = dst->max_pages;
+  a.lg_page = log2_of(ps), a.lc = log2_of((int32_t)(c->Dh / v));
+  a.heads_inner = c->Hkv > 1 && c->head_stride < c->token_stride;
+  const int64_t blocks = prune_blocks(&a);
+  if (blocks >= kMaxBlocks) return LAST_ERR_UNSUPPORTED;
+  return launch_cache_prune(a, blocks, (hipStream_t)stream) == hipSuccess ? LAST_OK : LAST_ERR_DEVICE;
+}
+
+last_status last_cache_copy(const last_cache *c, int32_t n, const int32_t *src, const int32_t *src_h,
+                            const int32_t *dst, const int32_t *dst_h, void *stream) {
+  const last_status st = check_cache(c);
+  if (st != LAST_OK) return st;
+  if (n < 0) return LAST_ERR_INVALID;
+  if (n == 0) return LAST_OK;
+  if (!src || !src_h || !dst || !dst_h) return LAST_ERR_INVALID;
+  {
+    PageSet read(c->n_pages), written(c->n_pages);
+    if (!read.ok() || !written.ok()) return LAST_ERR_UNSUPPORTED;
+    for (int32_t i = 0; i < n; ++i) {
+      if (src_h[i] < 0 || src_h[i] >= c->n_pages || dst_h[i] < 0 || dst_h[i] >= c->n_pages) return LAST_ERR_INVALID;
+      read.add(src_h[i]);
+    }
+    for (int32_t i = 0; i < n; ++i) {
+      if (read.has(dst_h[i]) || written.has(dst_h[i])) return LAST_ERR_INVALID;
+      written.add(dst_h[i]);
+    }
+  }
+  const int64_t v = piece_elems(c->dtype);
+  CopyArgs a{};
+  a.k = c->k, a.v = c->v, a.src = src, a.dst = dst;
+  a.layer_stride = c->layer_stride / v, a.page_stride = c->page_stride / v;
+  const bool heads_inner = c->Hkv > 1 && c->head_stride < c->token_stride;
+  a.inner = heads_inner ? c->Hkv : c->page_size;
+  a.inner_stride = (heads_inner ? c->head_stride : c->token_stride) / v;
+  a.outer_stride = (heads_inner ? c->token_stride : c->head_stride) / v;
+  a.n = n, a.G = c->G, a.n_pages = c->n_pages, a.lc = log2_of((int32_t)(c->Dh / v));
+  if ((int64_t)c->Hkv * c->page_size > (1 << 24)) return LAST_ERR_UNSUPPORTED;
+  a.pieces = (c->Hkv * c->page_size) << a.lc;
+  const int64_t blocks = copy_blocks(&a);
+  if (blocks >= kMaxBlocks) return LAST_ERR_UNSUPPORTED;
+  return launch_cache_copy(a, blocks, (hipStream_t)stream) == hipSuccess ? LAST_OK : LAST_ERR_DEVICE;
 }
 
 int32_t last_budget(int32_t N, int32_t rho_num, int32_t rho_den) {

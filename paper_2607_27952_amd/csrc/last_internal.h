@@ -280,6 +280,66 @@ hipError_t launch_connector(int64_t K, int32_t Dv, int32_t Dh, int32_t Do, float
                             const void *w2, const float *b2, void *out, void *xn, void *hid,
                             hipStream_t s);
 
+// ------------------------------------------------------------ rotary (rotary.hip)
+struct RotaryArgs {
+  const float *inv_freq;
+  const int32_t *axis, *pos;
+  int32_t F, adjacent, inverse;   // F = 0: nothing is turned
+  int32_t G, T, Hq, Hkv;
+  const void *q, *k, *v;
+  void *q_out, *k_out, *v_out;    // k_out, v_out: a cache's first layer when appending
+  int64_t q_ls, q_ts, k_ls, k_ts, v_ls, v_ts, qo_ls, qo_ts, ko_ls, ko_ts;
+  // appending
+  const int32_t *table, *lens, *cu_new;   // cu_new NULL: one token per sequence
+  int32_t R, max_pages, n_pages, lg_page, max_len;
+  int64_t page_stride, head_stride, slot_stride;
+  int32_t tokens, parts;          // of a block; blocks of a group of tokens (set by the launcher)
+};
+int64_t rotary_blocks(RotaryArgs a, bool append);
+hipError_t launch_rotary(RotaryArgs a, last_dtype dtype, int32_t Dh, bool append, hipStream_t s);
+
+// ------------------------------------------------------------ decode (decode.hip)
+constexpr int kDecodeIds = 1024;   // page ids a block holds
+struct DecodePlan {
+  int32_t keys, parts, head_tiles, max_len;   // keys of a part, parts of the longest sequence
+  int64_t blocks;
+};
+struct DecodeArgs {
+  const void *k, *v, *q;
+  void *out;
+  float *lse, *part_o;
+  float2 *part_ml;
+  const int32_t *table, *lens;
+  int64_t page_stride, head_stride, token_stride, q_stride;
+  int32_t R, Hq, Hkv, group, max_pages, n_pages, lg_page;
+  int32_t keys, parts, head_tiles, max_len;
+  float scale_log2;
+};
+DecodePlan make_decode_plan(const last_cache *c, const last_pages *p, int32_t Hq);
+hipError_t launch_decode(const DecodeArgs &a, last_dtype dtype, int32_t Dh, hipStream_t s);
+
+// ------------------------------------------------------------ pages (cache.hip)
+// Strides in 16-byte pieces; a row of Dh elements is 1 << lc pieces.
+struct CopyArgs {
+  void *k, *v;
+  const int32_t *src, *dst;
+  int64_t layer_stride, page_stride, inner_stride, outer_stride;
+  int32_t n, G, n_pages, lc, inner, pieces, chunks;   // inner rows; pieces of a page; blocks of it
+};
+int64_t copy_blocks(CopyArgs *a);
+hipError_t launch_cache_copy(const CopyArgs &a, int64_t blocks, hipStream_t s);
+
+struct PruneArgs {
+  void *k, *v;
+  const int32_t *src, *dst, *lens, *vis_start, *cu_vis, *kept, *cu_keep;
+  int32_t *new_lens;
+  int64_t layer_stride, page_stride, head_stride, token_stride;
+  int32_t R, G, Hkv, n_pages, src_pages, dst_pages, lg_page, lc, heads_inner;
+  int32_t max_old, max_new, tiles;
+};
+int64_t prune_blocks(PruneArgs *a);
+hipError_t launch_cache_prune(const PruneArgs &a, int64_t blocks, hipStream_t s);
+
 }  // namespace last
 
 // ----------------------------------------------------------------- device side

@@ -27,7 +27,9 @@ SRC_LAST, SRC_FIRST, SRC_MIDDLE, SRC_ALL_MEAN = 0, 1, 2, 3
 EXPORTS = ("last_token_scores_workspace", "last_token_scores", "last_token_scores_static", "last_source_rows",
            "last_rows_scores_workspace", "last_rows_scores", "last_prefill_attention_workspace",
            "last_prefill_attention", "diverse_select_workspace", "diverse_select_similarity_workspace",
-           "diverse_select", "diverse_select_similarity", "diverse_select_pick", "gather_kept", "last_connector_workspace", "last_connector", "last_budget", "last_status_string", "last_version",
+           "diverse_select", "diverse_select_similarity", "diverse_select_pick", "gather_kept", "last_connector_workspace", "last_connector",
+           "last_rotary", "last_rotary_append", "last_decode_attention_workspace", "last_decode_attention",
+           "last_cache_prune", "last_cache_copy", "last_budget", "last_status_string", "last_version",
            "last_profile_enable", "last_profile_collect", "last_profile_reset",
            "last_profile_count", "last_profile_kernel")
 
@@ -45,6 +47,28 @@ class _Batch(ctypes.Structure):
                 ("cu_seqlens", ctypes.c_void_p), ("cu_seqlens_h", ctypes.c_void_p),
                 ("vis_start", ctypes.c_void_p), ("vis_start_h", ctypes.c_void_p),
                 ("cu_vis", ctypes.c_void_p), ("cu_vis_h", ctypes.c_void_p)]
+
+
+class _Cache(ctypes.Structure):
+    _fields_ = [("G", ctypes.c_int32), ("n_pages", ctypes.c_int32), ("page_size", ctypes.c_int32),
+                ("Hkv", ctypes.c_int32), ("Dh", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("layer_stride", ctypes.c_int64), ("page_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64),
+                ("token_stride", ctypes.c_int64), ("k", ctypes.c_void_p), ("v", ctypes.c_void_p)]
+
+
+class _Pages(ctypes.Structure):
+    _fields_ = [("R", ctypes.c_int32), ("max_pages", ctypes.c_int32), ("table", ctypes.c_void_p),
+                ("table_h", ctypes.c_void_p), ("lens", ctypes.c_void_p), ("lens_h", ctypes.c_void_p)]
+
+
+class _Rotation(ctypes.Structure):
+    _fields_ = [("n_axes", ctypes.c_int32), ("n_freqs", ctypes.c_int32), ("adjacent", ctypes.c_int32),
+                ("inverse", ctypes.c_int32), ("inv_freq", ctypes.c_void_p), ("axis", ctypes.c_void_p),
+                ("axis_h", ctypes.c_void_p)]
+
+
+class _Heads(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("layer_stride", ctypes.c_int64), ("token_stride", ctypes.c_int64)]
 
 
 _lib = None
@@ -92,6 +116,20 @@ def lib():
         L.last_connector_workspace.restype = SZ
         L.last_connector.argtypes = [I32, I64, I32, I32, I32, ctypes.c_float, P, P, P, P, P, P, P, P, P, SZ, P]
         L.last_connector.restype = I32
+        PH = ctypes.POINTER(_Heads)
+        PC, PP, PR = ctypes.POINTER(_Cache), ctypes.POINTER(_Pages), ctypes.POINTER(_Rotation)
+        L.last_rotary.argtypes = [PR, I32, I32, I32, I32, I32, I32, P, PH, PH, PH, PH, P]
+        L.last_rotary.restype = I32
+        L.last_rotary_append.argtypes = [PR, PC, I32, I32, PP, I32, P, P, I32, P, PH, PH, PH, PH, P]
+        L.last_rotary_append.restype = I32
+        L.last_decode_attention_workspace.argtypes = [PC, PP, I32]
+        L.last_decode_attention_workspace.restype = SZ
+        L.last_decode_attention.argtypes = [PC, I32, PP, I32, ctypes.c_float, P, I64, P, P, P, SZ, P]
+        L.last_decode_attention.restype = I32
+        L.last_cache_prune.argtypes = [PC, PP, PP, P, P, P, P, P, P, P, P, P]
+        L.last_cache_prune.restype = I32
+        L.last_cache_copy.argtypes = [PC, I32, P, P, P, P, P]
+        L.last_cache_copy.restype = I32
         L.last_budget.argtypes = [I32, I32, I32]
         L.last_budget.restype = I32
         L.last_status_string.argtypes = [I32]
@@ -459,6 +497,295 @@ def connector(x: torch.Tensor, gamma: torch.Tensor, beta: torch.Tensor, w1: torc
         if st != LAST_OK:
             raise LastError(st, "last_connector")
         return out
+
+
+# ------------------------------------------------------------------ paged cache
+def _on_device(device, stream):
+    """The tensors' device and the call's stream made current for its allocations and launches."""
+    if device.type != "cuda":
+        raise ValueError(f"tensors must be on a GPU, got {device}")
+    stack = contextlib.ExitStack()
+    if device.index is not None and device.index != torch.cuda.current_device():
+        stack.enter_context(torch.cuda.device(device))
+    if stream is not None:
+        stack.enter_context(torch.cuda.stream(stream))
+    return stack
+
+
+def _dev_i32(t: torch.Tensor, device, what: str, shape=None) -> None:
+    if t.dtype != torch.int32 or t.device != device or not t.is_contiguous():
+        raise ValueError(f"{what} must be contiguous int32 on {device}")
+    if shape is not None and tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{what} must have the shape {tuple(shape)}")
+
+
+def _host_i32(a, what: str, shape=None) -> np.ndarray:
+    a = np.ascontiguousarray(a, dtype=np.int32)
+    if shape is not None and a.shape != tuple(shape):
+        raise ValueError(f"{what} must have the shape {tuple(shape)}")
+    return a
+
+
+@dataclass(frozen=True, eq=False)
+class Cache:
+    """A paged cache: k and v as [G][pages][Hkv][page_size][Dh], views of any stride order."""
+    k: torch.Tensor
+    v: torch.Tensor
+
+    def __post_init__(self):
+        k, v = self.k, self.v
+        if k.dim() != 5 or k.shape != v.shape or k.stride() != v.stride():
+            raise ValueError("k and v must be [G][pages][Hkv][page_size][Dh] with the same strides")
+        if k.dtype != v.dtype or k.device != v.device:
+            raise ValueError("k and v must share a dtype and a device")
+        if k.stride(4) != 1:
+            raise ValueError("the elements of a head must be contiguous")
+        G, n, H, ps, D = k.shape
+        ls, pg, hs, ts, _ = k.stride()
+        object.__setattr__(self, "_struct", _Cache(G, n, ps, H, D, _dtype_code(k), ls, pg, hs, ts, _ptr(k), _ptr(v)))
+
+    @staticmethod
+    def make(G, n_pages, page_size, Hkv, Dh, dtype=torch.bfloat16, device="cuda") -> "Cache":
+        shape = (G, n_pages, Hkv, page_size, Dh)
+        return Cache(torch.empty(shape, dtype=dtype, device=device), torch.empty(shape, dtype=dtype, device=device))
+
+    @property
+    def device(self):
+        return self.k.device
+
+
+@dataclass(frozen=True, eq=False)
+class Pages:
+    """The sequences of a cache: their page table [R][max_pages] and lengths [R], on host and device. The
+    device tensors may change between calls (in place); lens_h bounds lens, table_h may be None where the
+    call allows it."""
+    lens_h: np.ndarray
+    table: torch.Tensor
+    lens: torch.Tensor
+    table_h: Optional[np.ndarray] = None
+
+    def __post_init__(self):
+        if self.table.dim() != 2:
+            raise ValueError("table must be [R][max_pages]")
+        R, m = self.table.shape
+        dev = self.table.device
+        _dev_i32(self.table, dev, "table")
+        _dev_i32(self.lens, dev, "lens", (R,))
+        object.__setattr__(self, "lens_h", _host_i32(self.lens_h, "lens_h", (R,)))
+        if self.table_h is not None:
+            object.__setattr__(self, "table_h", _host_i32(self.table_h, "table_h", (R, m)))
+        object.__setattr__(self, "_struct", _Pages(R, m, _ptr(self.table), _ptr(self.table_h), _ptr(self.lens),
+                                                   _ptr(self.lens_h)))
+
+    @staticmethod
+    def make(table, lens, device="cuda") -> "Pages":
+        t, n = _i32_host(table), _i32_host(lens)
+        return Pages(table_h=t, lens_h=n, table=_i32_dev(t, device), lens=_i32_dev(n, device))
+
+    @property
+    def R(self) -> int:
+        return self.table.shape[0]
+
+
+@dataclass(frozen=True, eq=False)
+class Rotary:
+    """A rotation: inv_freq [F] fp32 and the position axis of each frequency."""
+    inv_freq: torch.Tensor
+    axis: torch.Tensor
+    axis_h: np.ndarray
+    n_axes: int = 1
+    adjacent: bool = False
+
+    def __post_init__(self):
+        F = self.inv_freq.numel()
+        if self.inv_freq.dtype != torch.float32 or not self.inv_freq.is_contiguous():
+            raise ValueError("inv_freq must be contiguous float32")
+        _dev_i32(self.axis, self.inv_freq.device, "axis", (F,))
+        object.__setattr__(self, "axis_h", _host_i32(self.axis_h, "axis_h", (F,)))
+        object.__setattr__(self, "_structs", tuple(
+            _Rotation(self.n_axes, F, int(self.adjacent), inverse, _ptr(self.inv_freq), _ptr(self.axis),
+                      _ptr(self.axis_h)) for inverse in (0, 1)))
+
+    @staticmethod
+    def make(inv_freq, sections=None, axis=None, adjacent=False, device="cuda") -> "Rotary":
+        """sections: how many frequencies, one after the other, turn by each axis; or axis: the axis of each."""
+        f = torch.as_tensor(inv_freq, dtype=torch.float32).to(device).contiguous()
+        if axis is None:
+            sections = [f.numel()] if sections is None else list(sections)
+            if sum(sections) != f.numel():
+                raise ValueError("sections must add up to the number of frequencies")
+            axis, n = np.repeat(np.arange(len(sections)), sections), len(sections)
+        else:
+            n = int(np.max(axis)) + 1
+        a = _i32_host(axis)
+        return Rotary(inv_freq=f, axis=_i32_dev(a, device), axis_h=a, n_axes=n, adjacent=bool(adjacent))
+
+
+def _heads(t: Optional[torch.Tensor], like: Optional[torch.Tensor] = None, what: str = "rows"):
+    """t [G][T][H][Dh] as last_heads (None where it has no rows)."""
+    if t is None:
+        return None
+    if t.dim() != 4 or t.stride(3) != 1 or (t.shape[2] > 1 and t.stride(2) != t.shape[3]):
+        raise ValueError(f"{what} must be [G][T][heads][Dh] with contiguous heads")
+    if like is not None and (t.shape != like.shape or t.dtype != like.dtype or t.device != like.device):
+        raise ValueError(f"{what} must have the shape, dtype and device of what it is computed from")
+    return _Heads(_ptr(t), t.stride(0), t.stride(1))
+
+
+def _positions(pos: torch.Tensor, rot: Rotary, T: int, device) -> torch.Tensor:
+    pos = pos[None] if pos.dim() == 1 else pos
+    _dev_i32(pos, device, "pos", (rot.n_axes, T))
+    if rot.inv_freq.device != device:
+        raise ValueError(f"the rotation must be on {device}")
+    return pos
+
+
+def rotary(rot: Rotary, pos: torch.Tensor, q: Optional[torch.Tensor], k: Optional[torch.Tensor] = None, q_out=None,
+           k_out=None, inverse=False, stream=None):
+    """last_rotary: q and k [G][T][heads][Dh] turned by pos [n_axes][T] (or [T]); inverse is the gradient.
+    Returns (q_out, k_out), None for what is not given; q_out may be q and k_out k."""
+    x = q if q is not None else k
+    if x is None:
+        raise ValueError("q or k is needed")
+    with _on_device(x.device, stream):
+        code = _dtype_code(x)
+        if q is not None and k is not None and (q.dtype != k.dtype or q.device != k.device or q.shape[:2] != k.shape[:2]
+                                                or q.shape[3] != k.shape[3]):
+            raise ValueError("q and k must share a dtype, a device, layers, tokens and the head dimension")
+        hq, hk = _heads(q, what="q"), _heads(k, what="k")
+        G, T, _, D = x.shape
+        pos = _positions(pos, rot, T, x.device)
+        if q is not None and q_out is None:
+            q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        if k is not None and k_out is None:
+            k_out = torch.empty(k.shape, dtype=k.dtype, device=k.device)
+        st = lib().last_rotary(rot._structs[1 if inverse else 0], code, G, T, q.shape[2] if q is not None else 0,
+                               k.shape[2] if k is not None else 0, D, _ptr(pos), hq, hk,
+                               _heads(q_out, q, "q_out") if q is not None else None,
+                               _heads(k_out, k, "k_out") if k is not None else None, _stream(stream))
+        if st != LAST_OK:
+            raise LastError(st, "last_rotary")
+        return q_out, k_out
+
+
+def rotary_append(rot: Optional[Rotary], cache: Cache, pages: Pages, pos: Optional[torch.Tensor],
+                  q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor, cu_new_h=None, cu_new=None, q_out=None,
+                  layer: int = 0, stream=None):
+    """last_rotary_append: k [G][T][Hkv][Dh] turned, and v, put into the cache's layers from `layer` on as the
+    last tokens of their sequences (pages.lens counts them already); q turned. Without cu_new_h every sequence
+    has one new token. rot None stores k as it is (q must be None). Returns q_out."""
+    dev = cache.device
+    with _on_device(dev, stream):
+        hk = _heads(k, what="k")
+        if k.dtype != cache.k.dtype or k.device != dev or k.shape[2:] != (cache.k.shape[2], cache.k.shape[4]):
+            raise ValueError("k must match the cache in dtype, device, heads and head dimension")
+        hv = _heads(v, k, "v")
+        G, T = k.shape[:2]
+        if pages.table.device != dev:
+            raise ValueError(f"the page table must be on {dev}")
+        hq = ho = None
+        if q is not None:
+            if q.dtype != k.dtype or q.device != dev or q.shape[:2] != k.shape[:2] or q.shape[3] != k.shape[3]:
+                raise ValueError("q must match k in dtype, device, layers, tokens and the head dimension")
+            hq = _heads(q, what="q")
+            if q_out is None:
+                q_out = torch.empty(q.shape, dtype=q.dtype, device=dev)
+            ho = _heads(q_out, q, "q_out")
+        if rot is not None:
+            if pos is None:
+                raise ValueError("a rotation needs positions")
+            pos = _positions(pos, rot, T, dev)
+        cu = None
+        if cu_new_h is not None:
+            cu = _host_i32(cu_new_h, "cu_new_h", (pages.R + 1,))
+            if cu_new is None:
+                cu_new = _i32_dev(cu, dev)
+            _dev_i32(cu_new, dev, "cu_new", (pages.R + 1,))
+        elif cu_new is not None:
+            raise ValueError("cu_new needs cu_new_h")
+        st = lib().last_rotary_append(rot._structs[0] if rot is not None else None, cache._struct, layer, G,
+                                      pages._struct, T, _ptr(cu_new), _ptr(cu), q.shape[2] if q is not None else 0,
+                                      _ptr(pos) if rot is not None else None, hq, ho, hk, hv, _stream(stream))
+        if st != LAST_OK:
+            raise LastError(st, "last_rotary_append")
+        return q_out
+
+
+def decode_attention_workspace(cache: Cache, pages: Pages, Hq: int) -> int:
+    return int(lib().last_decode_attention_workspace(cache._struct, pages._struct, int(Hq)))
+
+
+def decode_attention(cache: Cache, pages: Pages, q: torch.Tensor, layer: int = 0, scale: float = 0.0, out=None,
+                     lse=None, want_lse=False, ws=None, stream=None):
+    """last_decode_attention: q [R][Hq][Dh], one new token per sequence, over its cached tokens; returns
+    out [R][Hq][Dh] (and lse [R][Hq] fp32 if asked)."""
+    dev = cache.device
+    with _on_device(dev, stream):
+        if q.dim() != 3 or q.dtype != cache.k.dtype or q.device != dev or pages.table.device != dev:
+            raise ValueError("q must be [R][Hq][Dh], and q and the page table match the cache in dtype and device")
+        R, Hq, D = q.shape
+        if R != pages.R or D != cache.k.shape[4] or q.stride(2) != 1 or (Hq > 1 and q.stride(1) != D):
+            raise ValueError("q must have a row of contiguous heads for every sequence")
+        if out is None:
+            out = torch.empty((R, Hq, D), dtype=q.dtype, device=dev)
+        elif out.shape != q.shape or out.dtype != q.dtype or out.device != dev or not out.is_contiguous():
+            raise ValueError("out must be contiguous, with q's shape and dtype")
+        if want_lse and lse is None:
+            lse = torch.empty((R, Hq), dtype=torch.float32, device=dev)
+        if lse is not None and (lse.shape != (R, Hq) or lse.dtype != torch.float32 or lse.device != dev
+                                or not lse.is_contiguous()):
+            raise ValueError("lse must be contiguous float32 [R][Hq]")
+        if ws is None:
+            ws = _workspace(decode_attention_workspace(cache, pages, Hq), dev)
+        st = lib().last_decode_attention(cache._struct, layer, pages._struct, Hq, float(scale), _ptr(q), q.stride(0),
+                                         _ptr(out), _ptr(lse), _ptr(ws), ws.numel() * ws.element_size(),
+                                         _stream(stream))
+        if st != LAST_OK:
+            raise LastError(st, "last_decode_attention")
+        return (out, lse) if lse is not None else out
+
+
+def cache_prune(cache: Cache, src: Pages, dst: Pages, vis_start_h, cu_vis_h, kept: torch.Tensor, cu_keep_h,
+                vis_start=None, cu_vis=None, cu_keep=None, new_lens=None, stream=None) -> torch.Tensor:
+    """last_cache_prune (Eq. 12 on a cache): the text and the kept visual tokens of every sequence, in every layer,
+    from src's pages into dst's. The new lengths go to new_lens (dst.lens by default), which is returned."""
+    dev = cache.device
+    with _on_device(dev, stream):
+        R = src.R
+        vs, cv, ck = (_host_i32(vis_start_h, "vis_start_h", (R,)), _host_i32(cu_vis_h, "cu_vis_h", (R + 1,)),
+                      _host_i32(cu_keep_h, "cu_keep_h", (R + 1,)))
+        vis_start = _i32_dev(vs, dev) if vis_start is None else vis_start
+        cu_vis = _i32_dev(cv, dev) if cu_vis is None else cu_vis
+        cu_keep = _i32_dev(ck, dev) if cu_keep is None else cu_keep
+        new_lens = dst.lens if new_lens is None else new_lens
+        for t, what, n in ((vis_start, "vis_start", R), (cu_vis, "cu_vis", R + 1), (cu_keep, "cu_keep", R + 1),
+                           (new_lens, "new_lens", R)):
+            _dev_i32(t, dev, what, (n,))
+        _dev_i32(kept, dev, "kept")
+        if kept.numel() < int(ck[-1]) or src.table.device != dev or dst.table.device != dev:
+            raise ValueError("kept must hold cu_keep's indices, and the page tables be on the cache's device")
+        st = lib().last_cache_prune(cache._struct, src._struct, dst._struct, _ptr(vis_start), _ptr(vs), _ptr(cu_vis),
+                                    _ptr(cv), _ptr(kept), _ptr(cu_keep), _ptr(ck), _ptr(new_lens), _stream(stream))
+        if st != LAST_OK:
+            raise LastError(st, "last_cache_prune")
+        return new_lens
+
+
+def cache_copy(cache: Cache, src_h, dst_h, src=None, dst=None, stream=None) -> None:
+    """last_cache_copy: page src_h[i] copied to page dst_h[i], keys and values of every layer."""
+    dev = cache.device
+    with _on_device(dev, stream):
+        s = _host_i32(src_h, "src_h")
+        d = _host_i32(dst_h, "dst_h", s.shape)
+        if s.ndim != 1:
+            raise ValueError("src_h and dst_h must be one-dimensional")
+        src = _i32_dev(s, dev) if src is None else src
+        dst = _i32_dev(d, dev) if dst is None else dst
+        _dev_i32(src, dev, "src", s.shape)
+        _dev_i32(dst, dev, "dst", s.shape)
+        st = lib().last_cache_copy(cache._struct, len(s), _ptr(src), _ptr(s), _ptr(dst), _ptr(d), _stream(stream))
+        if st != LAST_OK:
+            raise LastError(st, "last_cache_copy")
 
 
 def budget(n: int, num: int, den: int) -> int:
