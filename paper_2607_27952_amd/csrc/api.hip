@@ -742,25 +742,24 @@ static last_status check_decode(const last_cache *c, const last_pages *p, int32_
   if ((st = check_pages(c, p, false)) != LAST_OK) return st;
   if (Hq < 1 || Hq % c->Hkv) return LAST_ERR_INVALID;
   *d = make_decode_plan(c, p, Hq);
-  if (d->blocks >= kMaxBlocks || (int64_t)p->R * Hq >= kMaxBlocks) return LAST_ERR_UNSUPPORTED;
+  if (d->blocks >= kMaxBlocks / 4 || (int64_t)p->R * Hq >= kMaxBlocks || d->steps >= (int64_t)1 << 31) return LAST_ERR_UNSUPPORTED;
   return LAST_OK;
 }
 
-static size_t decode_ws(const last_cache *c, const last_pages *p, int32_t Hq, const DecodePlan &d, void *ws,
-                        float **part_o, float2 **part_ml) {
+static size_t decode_ws(const last_cache *c, const last_pages *p, const DecodePlan &d, void *ws, DecodeArgs *a) {
   Carver cv(ws);
-  const size_t rows = d.parts > 1 ? (size_t)p->R * Hq * d.parts : 0;
-  float *o = cv.take<float>(rows * c->Dh);
-  float2 *ml = cv.take<float2>(rows);
-  if (part_o) *part_o = o;
-  if (part_ml) *part_ml = ml;
+  const size_t rows = d.split ? (size_t)d.blocks * 2 * d.heads_of_block * 16 : 0;   // two parts of a block
+  a->part_o = cv.take<float>(rows * c->Dh);
+  a->part_ml = cv.take<float2>(rows);
+  a->info = cv.take<int2>(d.split ? (size_t)p->R * (c->Hkv / d.heads_of_block) * d.head_tiles : 0);
   return std::max<size_t>(256, cv.size());
 }
 
 size_t last_decode_attention_workspace(const last_cache *c, const last_pages *p, int32_t Hq) {
   DecodePlan d;
   if (check_decode(c, p, Hq, &d) != LAST_OK) return 0;
-  return decode_ws(c, p, Hq, d, nullptr, nullptr, nullptr);
+  DecodeArgs a{};
+  return decode_ws(c, p, d, nullptr, &a);
 }
 
 last_status last_decode_attention(const last_cache *c, int32_t layer, const last_pages *p, int32_t Hq,
@@ -774,9 +773,9 @@ last_status last_decode_attention(const last_cache *c, int32_t layer, const last
   if (p->R > 1 && (q_stride < 0 || q_stride > kMaxStride / p->R || q_stride % piece_elems(c->dtype)))
     return LAST_ERR_INVALID;
   DecodeArgs a{};
-  const size_t need = decode_ws(c, p, Hq, d, nullptr, nullptr, nullptr);
+  const size_t need = decode_ws(c, p, d, nullptr, &a);
   if (!ws || ws_bytes < need || !aligned(ws, 256)) return LAST_ERR_WORKSPACE;
-  decode_ws(c, p, Hq, d, ws, &a.part_o, &a.part_ml);
+  decode_ws(c, p, d, ws, &a);
   const size_t e = c->dtype == LAST_BF16 ? 2 : 4, at = (size_t)(c->G > 1 ? layer * c->layer_stride : 0) * e;
   a.k = static_cast<const char *>(c->k) + at;
   a.v = static_cast<const char *>(c->v) + at;
@@ -786,7 +785,8 @@ last_status last_decode_attention(const last_cache *c, int32_t layer, const last
   a.q_stride = p->R > 1 ? q_stride : 0;
   a.R = p->R, a.Hq = Hq, a.Hkv = c->Hkv, a.group = Hq / c->Hkv;
   a.max_pages = p->max_pages, a.n_pages = c->n_pages, a.lg_page = log2_of(c->page_size);
-  a.keys = d.keys, a.parts = d.parts, a.head_tiles = d.head_tiles, a.max_len = d.max_len;
+  a.blocks = (int32_t)d.blocks, a.split = d.split, a.head_tiles = d.head_tiles, a.max_len = d.max_len;
+  a.heads_of_block = d.heads_of_block;
   a.scale_log2 = (scale > 0.f ? scale : 1.0f / sqrtf((float)c->Dh)) * 1.4426950408889634f;
   return launch_decode(a, c->dtype, c->Dh, (hipStream_t)stream) == hipSuccess ? LAST_OK : LAST_ERR_DEVICE;
 }

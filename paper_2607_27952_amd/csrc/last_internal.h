@@ -301,18 +301,20 @@ hipError_t launch_rotary(RotaryArgs a, last_dtype dtype, int32_t Dh, bool append
 // ------------------------------------------------------------ decode (decode.hip)
 constexpr int kDecodeIds = 1024;   // page ids a block holds
 struct DecodePlan {
-  int32_t keys, parts, head_tiles, max_len;   // keys of a part, parts of the longest sequence
-  int64_t blocks;
+  int32_t head_tiles, max_len, heads_of_block;
+  bool split;              // the line of steps in equal shares, or a block per unit
+  int64_t blocks, steps;   // steps of the line if all sequences had the longest bound
 };
 struct DecodeArgs {
   const void *k, *v, *q;
   void *out;
   float *lse, *part_o;
-  float2 *part_ml;
+  float2 *part_ml;   // maximum and sum of a part's heads
+  int2 *info;        // of a unit: its first part's slot, its parts
   const int32_t *table, *lens;
   int64_t page_stride, head_stride, token_stride, q_stride;
   int32_t R, Hq, Hkv, group, max_pages, n_pages, lg_page;
-  int32_t keys, parts, head_tiles, max_len;
+  int32_t blocks, split, head_tiles, max_len, heads_of_block;
   float scale_log2;
 };
 DecodePlan make_decode_plan(const last_cache *c, const last_pages *p, int32_t Hq);
