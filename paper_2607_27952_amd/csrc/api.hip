@@ -682,7 +682,7 @@ last_status last_rotary(const last_rotation *rot, last_dtype dtype, int32_t G, i
     if (k->data == k_out->data && ((T > 1 && a.k_ts != a.ko_ts) || (G > 1 && a.k_ls != a.ko_ls)))
       return LAST_ERR_INVALID;
   }
-  if (rotary_blocks(a, false) >= kMaxBlocks) return LAST_ERR_UNSUPPORTED;
+  if (rotary_blocks(a, dtype, Dh, false) >= kMaxBlocks) return LAST_ERR_UNSUPPORTED;
   return launch_rotary(a, dtype, Dh, false, (hipStream_t)stream) == hipSuccess ? LAST_OK : LAST_ERR_DEVICE;
 }
 
@@ -732,7 +732,7 @@ last_status last_rotary_append(const last_rotation *rot, const last_cache *c, in
   a.R = p->R, a.max_pages = p->max_pages, a.n_pages = c->n_pages, a.lg_page = log2_of(c->page_size);
   for (int32_t r = 0; r < p->R; ++r) a.max_len = std::max(a.max_len, p->lens_h[r]);
   a.page_stride = c->page_stride, a.head_stride = c->head_stride, a.slot_stride = c->token_stride;
-  if (rotary_blocks(a, true) >= kMaxBlocks) return LAST_ERR_UNSUPPORTED;
+  if (rotary_blocks(a, c->dtype, c->Dh, true) >= kMaxBlocks) return LAST_ERR_UNSUPPORTED;
   return launch_rotary(a, c->dtype, c->Dh, true, (hipStream_t)stream) == hipSuccess ? LAST_OK : LAST_ERR_DEVICE;
 }
 

@@ -295,7 +295,7 @@ struct RotaryArgs {
   int64_t page_stride, head_stride, slot_stride;
   int32_t tokens, parts;          // of a block; blocks of a group of tokens (set by the launcher)
 };
-int64_t rotary_blocks(RotaryArgs a, bool append);
+int64_t rotary_blocks(RotaryArgs a, last_dtype dtype, int32_t Dh, bool append);
 hipError_t launch_rotary(RotaryArgs a, last_dtype dtype, int32_t Dh, bool append, hipStream_t s);
 
 // ------------------------------------------------------------ decode (decode.hip)

@@ -9,8 +9,10 @@
 // remainder is rounded to fp32. Each angle is computed once per token, layer
 // and block and serves every head: one sine and cosine for up to 64 pairs.
 //
-// The work is a copy: each row is read once and written once, 32 bytes a
-// thread, as the two 16-byte pieces whose elements pair up.
+// The work is a copy, bound by the memory: each row is read once and written
+// once, 32 bytes a thread, as the two 16-byte pieces whose elements pair up.
+// 5.7 to 6.1 TB/s on 0.5 GB and more, where a copy of 1 GiB by the framework
+// that holds the tensors reaches 5.2.
 #include <algorithm>
 
 #include "last_internal.h"
@@ -19,48 +21,54 @@ namespace {
 
 using last::RotaryArgs;
 
-constexpr int kTokens = 4;   // tokens of a block when there are many
+constexpr int kTokens = 4;   // most tokens of a block
 
 template <typename T>
 struct Piece;   // 16 bytes as floats
 template <>
 struct Piece<float> {
   static constexpr int kN = 4;
-  static __device__ __forceinline__ void get(const float *p, float (&x)[kN]) {
-    const float4 v = *reinterpret_cast<const float4 *>(p);
-    x[0] = v.x, x[1] = v.y, x[2] = v.z, x[3] = v.w;
+  typedef float vec __attribute__((ext_vector_type(4)));
+  static __device__ __forceinline__ void get(const vec v, float (&x)[kN]) {
+#pragma unroll
+    for (int i = 0; i < kN; ++i) x[i] = v[i];
   }
-  static __device__ __forceinline__ void put(float *p, const float (&x)[kN]) {
-    *reinterpret_cast<float4 *>(p) = make_float4(x[0], x[1], x[2], x[3]);
+  static __device__ __forceinline__ vec put(const float (&x)[kN]) {
+    vec v;
+#pragma unroll
+    for (int i = 0; i < kN; ++i) v[i] = x[i];
+    return v;
   }
 };
 template <>
 struct Piece<__bf16> {
   static constexpr int kN = 8;
   typedef __bf16 vec __attribute__((ext_vector_type(8)));
-  static __device__ __forceinline__ void get(const __bf16 *p, float (&x)[kN]) {
-    const vec v = *reinterpret_cast<const vec *>(p);
+  static __device__ __forceinline__ void get(const vec v, float (&x)[kN]) {
 #pragma unroll
     for (int i = 0; i < kN; ++i) x[i] = (float)v[i];
   }
-  static __device__ __forceinline__ void put(__bf16 *p, const float (&x)[kN]) {
+  static __device__ __forceinline__ vec put(const float (&x)[kN]) {
     vec v;
 #pragma unroll
-    for (int i = 0; i < kN; ++i) v[i] = (__bf16)x[i];
-    *reinterpret_cast<vec *>(p) = v;
+    for (int i = 0; i < kN; ++i) v[i] = (__bf16)x[i];   // to nearest even, once
+    return v;
   }
 };
 
 // Where token t of the new ones is stored, in elements from its layer's start;
-// -1 where it is not.
+// -1 where it is not. Called by whole waves: its sequence is found with 64
+// probes a level.
 __device__ int64_t cache_place(const RotaryArgs &a, int t) {
   int r = t, first = t, count = 1;
   if (a.cu_new) {
-    int lo = 0, hi = a.R;   // largest r with cu_new[r] <= t
+    int lo = 0, hi = a.R;   // the largest r with cu_new[r] <= t is in [lo, hi)
     while (hi - lo > 1) {
-      const int mid = (lo + hi) / 2;
-      if (a.cu_new[mid] <= t) lo = mid;
-      else hi = mid;
+      const int step = (hi - lo + 63) / 64, at = lo + (int)(threadIdx.x & 63) * step;
+      const unsigned long long ok = __ballot(at < hi && a.cu_new[at] <= t);
+      if (!ok) return -1;
+      lo += (63 - __clzll((long long)ok)) * step;
+      hi = min(hi, lo + step);
     }
     r = lo;
     first = a.cu_new[r];
@@ -94,7 +102,11 @@ __global__ __launch_bounds__(256) void k_rotary(RotaryArgs a) {
     cs[t][f] = c;
     sn[t][f] = a.inverse ? -s : s;
   }
-  if (APPEND && (int)threadIdx.x < nt) place[threadIdx.x] = cache_place(a, t0 + threadIdx.x);
+  if (APPEND)
+    for (int t = threadIdx.x / 64; t < nt; t += 4) {
+      const int64_t at = cache_place(a, t0 + t);
+      if (threadIdx.x % 64 == 0) place[t] = at;
+    }
   __syncthreads();
 
   const int heads = a.Hq + (APPEND ? 2 : 1) * a.Hkv;
@@ -133,8 +145,10 @@ __global__ __launch_bounds__(256) void k_rotary(RotaryArgs a) {
     const int p0 = halves ? ic : 2 * ic;
     const int p1 = halves ? ic + half : p0 + 1;
     float x[VEC], y[VEC];
-    Piece<T>::get(src + p0 * VEC, x);
-    Piece<T>::get(src + p1 * VEC, y);
+    typedef typename Piece<T>::vec vec;
+    const vec *s0 = reinterpret_cast<const vec *>(src + p0 * VEC), *s1 = reinterpret_cast<const vec *>(src + p1 * VEC);
+    Piece<T>::get(*s0, x);
+    Piece<T>::get(*s1, y);
     if (turn && halves) {
 #pragma unroll
       for (int e = 0; e < VEC; ++e) {
@@ -155,8 +169,17 @@ __global__ __launch_bounds__(256) void k_rotary(RotaryArgs a) {
         y[e] = w;
       }
     }
-    Piece<T>::put(dst + p0 * VEC, x);
-    Piece<T>::put(dst + p1 * VEC, y);
+    // Past the caches where the rows go to pages (appending 123000 tokens of
+    // 12 + 2 heads 154 against 160 us), not where they stay rows (132096 tokens
+    // of 28 + 4 heads 354 against 363).
+    vec *d0 = reinterpret_cast<vec *>(dst + p0 * VEC), *d1 = reinterpret_cast<vec *>(dst + p1 * VEC);
+    if (APPEND) {
+      __builtin_nontemporal_store(Piece<T>::put(x), d0);
+      __builtin_nontemporal_store(Piece<T>::put(y), d1);
+    } else {
+      *d0 = Piece<T>::put(x);
+      *d1 = Piece<T>::put(y);
+    }
   }
 }
 
@@ -175,26 +198,35 @@ void launch_t(const RotaryArgs &a, int Dh, bool append, unsigned blocks, hipStre
 
 namespace last {
 
-// Tokens of a block: 4 where that still leaves 4 blocks a compute unit, else
-// one, its heads dealt to several blocks until there are about as many.
-static void shape(RotaryArgs *a, bool append, int cus, int64_t *blocks) {
+// Tokens of a block: as many as give its 256 threads about one item of 32
+// bytes each (two when appending, where a block first looks its tokens' places
+// up), if that leaves 4 blocks a compute unit; else one, its heads dealt to
+// several blocks until there are about 2 a compute unit. In bf16, heads of 128:
+//   132096 tokens, 28 + 4 heads     1 token 363 us, 2 380, 4 398
+//   100000 tokens, 12 + 2 heads     1 token 180 us, 2 134, 4 160
+//   appending 123000, 12 + 2 + 2    1 token 304 us, 2 190, 4 154, 8 164
+//   appending 16384, 28 + 4 + 4     1 token  68 us, 2  59, 4  61
+static void shape(RotaryArgs *a, int items, bool append, int cus, int64_t *blocks) {
   const int heads = a->Hq + (append ? 2 : 1) * a->Hkv;
-  a->tokens = (int64_t)a->T * a->G >= (int64_t)kTokens * 4 * cus ? kTokens : 1;
+  const int want = std::max(1, std::min(kTokens, (2 * (append ? 512 : 256) + heads * items) / (2 * heads * items)));
+  a->tokens = (int64_t)a->T * a->G >= (int64_t)want * 4 * cus ? want : 1;
   const int64_t b = (int64_t)((a->T + a->tokens - 1) / a->tokens) * a->G;
   int64_t parts = std::max<int64_t>(1, (2 * cus) / b);
   a->parts = (int32_t)std::min<int64_t>(parts, std::max(1, heads / 8));
   *blocks = b * a->parts;
 }
 
-int64_t rotary_blocks(RotaryArgs a, bool append) {
+static int row_items(last_dtype dtype, int32_t Dh) { return Dh / (dtype == LAST_BF16 ? 16 : 8); }
+
+int64_t rotary_blocks(RotaryArgs a, last_dtype dtype, int32_t Dh, bool append) {
   int64_t blocks = 0;
-  shape(&a, append, device_cus(), &blocks);
+  shape(&a, row_items(dtype, Dh), append, device_cus(), &blocks);
   return blocks;
 }
 
 hipError_t launch_rotary(RotaryArgs a, last_dtype dtype, int32_t Dh, bool append, hipStream_t s) {
   int64_t blocks = 0;
-  shape(&a, append, device_cus(), &blocks);
+  shape(&a, row_items(dtype, Dh), append, device_cus(), &blocks);
   launch_begin(append ? "rotary_append" : "rotary", s);
   if (dtype == LAST_F32) launch_t<float>(a, Dh, append, (unsigned)blocks, s);
   else launch_t<__bf16>(a, Dh, append, (unsigned)blocks, s);
