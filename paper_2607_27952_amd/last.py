@@ -49,25 +49,32 @@ class _Batch(ctypes.Structure):
                 ("cu_vis", ctypes.c_void_p), ("cu_vis_h", ctypes.c_void_p)]
 
 
-class _Cache(ctypes.Structure):
+class _ByAddress(ctypes.Structure):
+    """A structure of the cache's calls: they take its address, which the handles below keep."""
+    @property
+    def _as_parameter_(self):
+        return ctypes.addressof(self)
+
+
+class _Cache(_ByAddress):
     _fields_ = [("G", ctypes.c_int32), ("n_pages", ctypes.c_int32), ("page_size", ctypes.c_int32),
                 ("Hkv", ctypes.c_int32), ("Dh", ctypes.c_int32), ("dtype", ctypes.c_int32),
                 ("layer_stride", ctypes.c_int64), ("page_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64),
                 ("token_stride", ctypes.c_int64), ("k", ctypes.c_void_p), ("v", ctypes.c_void_p)]
 
 
-class _Pages(ctypes.Structure):
+class _Pages(_ByAddress):
     _fields_ = [("R", ctypes.c_int32), ("max_pages", ctypes.c_int32), ("table", ctypes.c_void_p),
                 ("table_h", ctypes.c_void_p), ("lens", ctypes.c_void_p), ("lens_h", ctypes.c_void_p)]
 
 
-class _Rotation(ctypes.Structure):
+class _Rotation(_ByAddress):
     _fields_ = [("n_axes", ctypes.c_int32), ("n_freqs", ctypes.c_int32), ("adjacent", ctypes.c_int32),
                 ("inverse", ctypes.c_int32), ("inv_freq", ctypes.c_void_p), ("axis", ctypes.c_void_p),
                 ("axis_h", ctypes.c_void_p)]
 
 
-class _Heads(ctypes.Structure):
+class _Heads(_ByAddress):
     _fields_ = [("data", ctypes.c_void_p), ("layer_stride", ctypes.c_int64), ("token_stride", ctypes.c_int64)]
 
 
@@ -116,19 +123,18 @@ def lib():
         L.last_connector_workspace.restype = SZ
         L.last_connector.argtypes = [I32, I64, I32, I32, I32, ctypes.c_float, P, P, P, P, P, P, P, P, P, SZ, P]
         L.last_connector.restype = I32
-        PH = ctypes.POINTER(_Heads)
-        PC, PP, PR = ctypes.POINTER(_Cache), ctypes.POINTER(_Pages), ctypes.POINTER(_Rotation)
-        L.last_rotary.argtypes = [PR, I32, I32, I32, I32, I32, I32, P, PH, PH, PH, PH, P]
+        # structures of the cache's calls go by address
+        L.last_rotary.argtypes = [P, I32, I32, I32, I32, I32, I32, P, P, P, P, P, P]
         L.last_rotary.restype = I32
-        L.last_rotary_append.argtypes = [PR, PC, I32, I32, PP, I32, P, P, I32, P, PH, PH, PH, PH, P]
+        L.last_rotary_append.argtypes = [P, P, I32, I32, P, I32, P, P, I32, P, P, P, P, P, P]
         L.last_rotary_append.restype = I32
-        L.last_decode_attention_workspace.argtypes = [PC, PP, I32]
+        L.last_decode_attention_workspace.argtypes = [P, P, I32]
         L.last_decode_attention_workspace.restype = SZ
-        L.last_decode_attention.argtypes = [PC, I32, PP, I32, ctypes.c_float, P, I64, P, P, P, SZ, P]
+        L.last_decode_attention.argtypes = [P, I32, P, I32, ctypes.c_float, P, I64, P, P, P, SZ, P]
         L.last_decode_attention.restype = I32
-        L.last_cache_prune.argtypes = [PC, PP, PP, P, P, P, P, P, P, P, P, P]
+        L.last_cache_prune.argtypes = [P] * 12
         L.last_cache_prune.restype = I32
-        L.last_cache_copy.argtypes = [PC, I32, P, P, P, P, P]
+        L.last_cache_copy.argtypes = [P, I32, P, P, P, P, P]
         L.last_cache_copy.restype = I32
         L.last_budget.argtypes = [I32, I32, I32]
         L.last_budget.restype = I32
@@ -500,28 +506,39 @@ def connector(x: torch.Tensor, gamma: torch.Tensor, beta: torch.Tensor, w1: torc
 
 
 # ------------------------------------------------------------------ paged cache
-def _on_device(device, stream):
+# A decoding step makes these calls once per layer, with kernels of a few
+# microseconds: each checks what it is given once, cheaply, and the handles
+# (Cache, Pages, Rotary) keep their C structures.
+_HERE = contextlib.nullcontext()
+
+
+def _raw_stream(dev: int, stream) -> int:
+    return torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream
+
+
+def _on_device(dev: int, stream):
     """The tensors' device and the call's stream made current for its allocations and launches."""
-    if device.type != "cuda":
-        raise ValueError(f"tensors must be on a GPU, got {device}")
+    if dev < 0:
+        raise ValueError("tensors must be on a GPU")
+    if stream is None and dev == torch.cuda.current_device():
+        return _HERE
     stack = contextlib.ExitStack()
-    if device.index is not None and device.index != torch.cuda.current_device():
-        stack.enter_context(torch.cuda.device(device))
+    stack.enter_context(torch.cuda.device(dev))
     if stream is not None:
         stack.enter_context(torch.cuda.stream(stream))
     return stack
 
 
-def _dev_i32(t: torch.Tensor, device, what: str, shape=None) -> None:
-    if t.dtype != torch.int32 or t.device != device or not t.is_contiguous():
-        raise ValueError(f"{what} must be contiguous int32 on {device}")
-    if shape is not None and tuple(t.shape) != tuple(shape):
+def _dev_i32(t: torch.Tensor, dev: int, what: str, shape=None) -> None:
+    if t.dtype is not torch.int32 or t.get_device() != dev or not t.is_contiguous():
+        raise ValueError(f"{what} must be contiguous int32 on the device of the call")
+    if shape is not None and t.shape != shape:
         raise ValueError(f"{what} must have the shape {tuple(shape)}")
 
 
 def _host_i32(a, what: str, shape=None) -> np.ndarray:
     a = np.ascontiguousarray(a, dtype=np.int32)
-    if shape is not None and a.shape != tuple(shape):
+    if shape is not None and a.shape != shape:
         raise ValueError(f"{what} must have the shape {tuple(shape)}")
     return a
 
@@ -542,16 +559,15 @@ class Cache:
             raise ValueError("the elements of a head must be contiguous")
         G, n, H, ps, D = k.shape
         ls, pg, hs, ts, _ = k.stride()
-        object.__setattr__(self, "_struct", _Cache(G, n, ps, H, D, _dtype_code(k), ls, pg, hs, ts, _ptr(k), _ptr(v)))
+        c = _Cache(G, n, ps, H, D, _dtype_code(k), ls, pg, hs, ts, _ptr(k), _ptr(v))
+        for name, value in (("_struct", c), ("_at", ctypes.addressof(c)), ("_dev", k.get_device()), ("_dtype", k.dtype),
+                            ("_Hkv", H), ("_Dh", D)):
+            object.__setattr__(self, name, value)
 
     @staticmethod
     def make(G, n_pages, page_size, Hkv, Dh, dtype=torch.bfloat16, device="cuda") -> "Cache":
         shape = (G, n_pages, Hkv, page_size, Dh)
         return Cache(torch.empty(shape, dtype=dtype, device=device), torch.empty(shape, dtype=dtype, device=device))
-
-    @property
-    def device(self):
-        return self.k.device
 
 
 @dataclass(frozen=True, eq=False)
@@ -568,23 +584,20 @@ class Pages:
         if self.table.dim() != 2:
             raise ValueError("table must be [R][max_pages]")
         R, m = self.table.shape
-        dev = self.table.device
+        dev = self.table.get_device()
         _dev_i32(self.table, dev, "table")
         _dev_i32(self.lens, dev, "lens", (R,))
         object.__setattr__(self, "lens_h", _host_i32(self.lens_h, "lens_h", (R,)))
         if self.table_h is not None:
             object.__setattr__(self, "table_h", _host_i32(self.table_h, "table_h", (R, m)))
-        object.__setattr__(self, "_struct", _Pages(R, m, _ptr(self.table), _ptr(self.table_h), _ptr(self.lens),
-                                                   _ptr(self.lens_h)))
+        p = _Pages(R, m, _ptr(self.table), _ptr(self.table_h), _ptr(self.lens), _ptr(self.lens_h))
+        for name, value in (("_struct", p), ("_at", ctypes.addressof(p)), ("_dev", dev), ("R", R)):
+            object.__setattr__(self, name, value)
 
     @staticmethod
     def make(table, lens, device="cuda") -> "Pages":
         t, n = _i32_host(table), _i32_host(lens)
         return Pages(table_h=t, lens_h=n, table=_i32_dev(t, device), lens=_i32_dev(n, device))
-
-    @property
-    def R(self) -> int:
-        return self.table.shape[0]
 
 
 @dataclass(frozen=True, eq=False)
@@ -597,14 +610,15 @@ class Rotary:
     adjacent: bool = False
 
     def __post_init__(self):
-        F = self.inv_freq.numel()
+        F, dev = self.inv_freq.numel(), self.inv_freq.get_device()
         if self.inv_freq.dtype != torch.float32 or not self.inv_freq.is_contiguous():
             raise ValueError("inv_freq must be contiguous float32")
-        _dev_i32(self.axis, self.inv_freq.device, "axis", (F,))
+        _dev_i32(self.axis, dev, "axis", (F,))
         object.__setattr__(self, "axis_h", _host_i32(self.axis_h, "axis_h", (F,)))
-        object.__setattr__(self, "_structs", tuple(
-            _Rotation(self.n_axes, F, int(self.adjacent), inverse, _ptr(self.inv_freq), _ptr(self.axis),
-                      _ptr(self.axis_h)) for inverse in (0, 1)))
+        both = tuple(_Rotation(self.n_axes, F, int(self.adjacent), inverse, _ptr(self.inv_freq), _ptr(self.axis),
+                               _ptr(self.axis_h)) for inverse in (0, 1))
+        for name, value in (("_structs", both), ("_at", tuple(ctypes.addressof(x) for x in both)), ("_dev", dev)):
+            object.__setattr__(self, name, value)
 
     @staticmethod
     def make(inv_freq, sections=None, axis=None, adjacent=False, device="cuda") -> "Rotary":
@@ -621,23 +635,27 @@ class Rotary:
         return Rotary(inv_freq=f, axis=_i32_dev(a, device), axis_h=a, n_axes=n, adjacent=bool(adjacent))
 
 
-def _heads(t: Optional[torch.Tensor], like: Optional[torch.Tensor] = None, what: str = "rows"):
-    """t [G][T][H][Dh] as last_heads (None where it has no rows)."""
-    if t is None:
-        return None
-    if t.dim() != 4 or t.stride(3) != 1 or (t.shape[2] > 1 and t.stride(2) != t.shape[3]):
-        raise ValueError(f"{what} must be [G][T][heads][Dh] with contiguous heads")
-    if like is not None and (t.shape != like.shape or t.dtype != like.dtype or t.device != like.device):
-        raise ValueError(f"{what} must have the shape, dtype and device of what it is computed from")
-    return _Heads(_ptr(t), t.stride(0), t.stride(1))
+def _rows(t: torch.Tensor, dev: int, dtype, G: int, T: int, H, D: int, what: str):
+    """t [G][T][H][D] (H None: any) as the three numbers of a last_heads, and its heads."""
+    if t.dim() != 4 or t.dtype is not dtype or t.get_device() != dev:
+        raise ValueError(f"{what} must be [G][T][heads][Dh], of the dtype and on the device of the call")
+    g, n, h, d = t.shape
+    ls, ts, hs, es = t.stride()
+    if g != G or n != T or d != D or (H is not None and h != H) or es != 1 or (h > 1 and hs != D):
+        raise ValueError(f"{what} must be [{G}][{T}][{'heads' if H is None else H}][{D}] with contiguous heads")
+    return (t.data_ptr(), ls, ts), h
 
 
-def _positions(pos: torch.Tensor, rot: Rotary, T: int, device) -> torch.Tensor:
-    pos = pos[None] if pos.dim() == 1 else pos
-    _dev_i32(pos, device, "pos", (rot.n_axes, T))
-    if rot.inv_freq.device != device:
-        raise ValueError(f"the rotation must be on {device}")
-    return pos
+_FourHeads = ctypes.c_int64 * 12   # four last_heads
+_NO_HEADS = (0, 0, 0)
+
+
+def _positions(pos: torch.Tensor, rot: Rotary, T: int, dev: int) -> int:
+    if pos.dtype is not torch.int32 or pos.get_device() != dev or rot._dev != dev or not pos.is_contiguous():
+        raise ValueError("pos must be contiguous int32, and it and the rotation be on the device of the call")
+    if pos.shape != (rot.n_axes, T) and not (rot.n_axes == 1 and pos.shape == (T,)):
+        raise ValueError(f"pos must have the shape {(rot.n_axes, T)}")
+    return pos.data_ptr()
 
 
 def rotary(rot: Rotary, pos: torch.Tensor, q: Optional[torch.Tensor], k: Optional[torch.Tensor] = None, q_out=None,
@@ -645,27 +663,35 @@ def rotary(rot: Rotary, pos: torch.Tensor, q: Optional[torch.Tensor], k: Optiona
     """last_rotary: q and k [G][T][heads][Dh] turned by pos [n_axes][T] (or [T]); inverse is the gradient.
     Returns (q_out, k_out), None for what is not given; q_out may be q and k_out k."""
     x = q if q is not None else k
-    if x is None:
-        raise ValueError("q or k is needed")
-    with _on_device(x.device, stream):
+    if x is None or x.dim() != 4:
+        raise ValueError("q or k is needed, as [G][T][heads][Dh]")
+    dev, dtype = x.get_device(), x.dtype
+    with _on_device(dev, stream):
         code = _dtype_code(x)
-        if q is not None and k is not None and (q.dtype != k.dtype or q.device != k.device or q.shape[:2] != k.shape[:2]
-                                                or q.shape[3] != k.shape[3]):
-            raise ValueError("q and k must share a dtype, a device, layers, tokens and the head dimension")
-        hq, hk = _heads(q, what="q"), _heads(k, what="k")
         G, T, _, D = x.shape
-        pos = _positions(pos, rot, T, x.device)
-        if q is not None and q_out is None:
-            q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-        if k is not None and k_out is None:
-            k_out = torch.empty(k.shape, dtype=k.dtype, device=k.device)
-        st = lib().last_rotary(rot._structs[1 if inverse else 0], code, G, T, q.shape[2] if q is not None else 0,
-                               k.shape[2] if k is not None else 0, D, _ptr(pos), hq, hk,
-                               _heads(q_out, q, "q_out") if q is not None else None,
-                               _heads(k_out, k, "k_out") if k is not None else None, _stream(stream))
-        if st != LAST_OK:
-            raise LastError(st, "last_rotary")
-        return q_out, k_out
+        at = _positions(pos, rot, T, dev)
+        rows, heads = [], []
+        for t, out, what in ((q, q_out, "q"), (k, k_out, "k")):
+            if t is None:
+                rows += [_NO_HEADS, _NO_HEADS]
+                heads.append(0)
+                continue
+            r, h = _rows(t, dev, dtype, G, T, None, D, what)
+            if out is None:
+                out = torch.empty((G, T, h, D), dtype=dtype, device=t.device)
+                if what == "q":
+                    q_out = out
+                else:
+                    k_out = out
+            rows += [r, _rows(out, dev, dtype, G, T, h, D, what + "_out")[0]]
+            heads.append(h)
+        h4 = _FourHeads(*rows[0], *rows[1], *rows[2], *rows[3])
+        p = ctypes.addressof(h4)
+        st = lib().last_rotary(rot._at[1 if inverse else 0], code, G, T, heads[0], heads[1], D, at, p, p + 48, p + 24,
+                               p + 72, _raw_stream(dev, stream))
+    if st != LAST_OK:
+        raise LastError(st, "last_rotary")
+    return q_out if q is not None else None, k_out if k is not None else None
 
 
 def rotary_append(rot: Optional[Rotary], cache: Cache, pages: Pages, pos: Optional[torch.Tensor],
@@ -674,118 +700,122 @@ def rotary_append(rot: Optional[Rotary], cache: Cache, pages: Pages, pos: Option
     """last_rotary_append: k [G][T][Hkv][Dh] turned, and v, put into the cache's layers from `layer` on as the
     last tokens of their sequences (pages.lens counts them already); q turned. Without cu_new_h every sequence
     has one new token. rot None stores k as it is (q must be None). Returns q_out."""
-    dev = cache.device
+    dev, dtype, D = cache._dev, cache._dtype, cache._Dh
     with _on_device(dev, stream):
-        hk = _heads(k, what="k")
-        if k.dtype != cache.k.dtype or k.device != dev or k.shape[2:] != (cache.k.shape[2], cache.k.shape[4]):
-            raise ValueError("k must match the cache in dtype, device, heads and head dimension")
-        hv = _heads(v, k, "v")
+        if k.dim() != 4 or pages._dev != dev:
+            raise ValueError("k must be [G][T][Hkv][Dh], and the page table on the cache's device")
         G, T = k.shape[:2]
-        if pages.table.device != dev:
-            raise ValueError(f"the page table must be on {dev}")
-        hq = ho = None
+        kr, _ = _rows(k, dev, dtype, G, T, cache._Hkv, D, "k")
+        vr, _ = _rows(v, dev, dtype, G, T, cache._Hkv, D, "v")
+        qr = qo = _NO_HEADS
+        Hq = at = 0
         if q is not None:
-            if q.dtype != k.dtype or q.device != dev or q.shape[:2] != k.shape[:2] or q.shape[3] != k.shape[3]:
-                raise ValueError("q must match k in dtype, device, layers, tokens and the head dimension")
-            hq = _heads(q, what="q")
+            qr, Hq = _rows(q, dev, dtype, G, T, None, D, "q")
             if q_out is None:
-                q_out = torch.empty(q.shape, dtype=q.dtype, device=dev)
-            ho = _heads(q_out, q, "q_out")
+                q_out = torch.empty((G, T, Hq, D), dtype=dtype, device=q.device)
+            qo, _ = _rows(q_out, dev, dtype, G, T, Hq, D, "q_out")
         if rot is not None:
             if pos is None:
                 raise ValueError("a rotation needs positions")
-            pos = _positions(pos, rot, T, dev)
+            at = _positions(pos, rot, T, dev)
         cu = None
         if cu_new_h is not None:
             cu = _host_i32(cu_new_h, "cu_new_h", (pages.R + 1,))
             if cu_new is None:
-                cu_new = _i32_dev(cu, dev)
+                cu_new = _i32_dev(cu, cache.k.device)
             _dev_i32(cu_new, dev, "cu_new", (pages.R + 1,))
         elif cu_new is not None:
             raise ValueError("cu_new needs cu_new_h")
-        st = lib().last_rotary_append(rot._structs[0] if rot is not None else None, cache._struct, layer, G,
-                                      pages._struct, T, _ptr(cu_new), _ptr(cu), q.shape[2] if q is not None else 0,
-                                      _ptr(pos) if rot is not None else None, hq, ho, hk, hv, _stream(stream))
-        if st != LAST_OK:
-            raise LastError(st, "last_rotary_append")
-        return q_out
+        h4 = _FourHeads(*qr, *qo, *kr, *vr)
+        p = ctypes.addressof(h4)
+        st = lib().last_rotary_append(rot._at[0] if rot is not None else None, cache._at, layer, G, pages._at, T,
+                                      _ptr(cu_new), _ptr(cu), Hq, at, p, p + 24, p + 48, p + 72, _raw_stream(dev, stream))
+    if st != LAST_OK:
+        raise LastError(st, "last_rotary_append")
+    return q_out
 
 
 def decode_attention_workspace(cache: Cache, pages: Pages, Hq: int) -> int:
-    return int(lib().last_decode_attention_workspace(cache._struct, pages._struct, int(Hq)))
+    return int(lib().last_decode_attention_workspace(cache._at, pages._at, int(Hq)))
 
 
 def decode_attention(cache: Cache, pages: Pages, q: torch.Tensor, layer: int = 0, scale: float = 0.0, out=None,
                      lse=None, want_lse=False, ws=None, stream=None):
     """last_decode_attention: q [R][Hq][Dh], one new token per sequence, over its cached tokens; returns
     out [R][Hq][Dh] (and lse [R][Hq] fp32 if asked)."""
-    dev = cache.device
+    dev, dtype, D = cache._dev, cache._dtype, cache._Dh
     with _on_device(dev, stream):
-        if q.dim() != 3 or q.dtype != cache.k.dtype or q.device != dev or pages.table.device != dev:
+        if q.dim() != 3 or q.dtype is not dtype or q.get_device() != dev or pages._dev != dev:
             raise ValueError("q must be [R][Hq][Dh], and q and the page table match the cache in dtype and device")
-        R, Hq, D = q.shape
-        if R != pages.R or D != cache.k.shape[4] or q.stride(2) != 1 or (Hq > 1 and q.stride(1) != D):
+        R, Hq, d = q.shape
+        rs, hs, es = q.stride()
+        if R != pages.R or d != D or es != 1 or (Hq > 1 and hs != D):
             raise ValueError("q must have a row of contiguous heads for every sequence")
         if out is None:
-            out = torch.empty((R, Hq, D), dtype=q.dtype, device=dev)
-        elif out.shape != q.shape or out.dtype != q.dtype or out.device != dev or not out.is_contiguous():
+            out = torch.empty((R, Hq, D), dtype=dtype, device=q.device)
+        elif out.shape != q.shape or out.dtype is not dtype or out.get_device() != dev or not out.is_contiguous():
             raise ValueError("out must be contiguous, with q's shape and dtype")
-        if want_lse and lse is None:
-            lse = torch.empty((R, Hq), dtype=torch.float32, device=dev)
-        if lse is not None and (lse.shape != (R, Hq) or lse.dtype != torch.float32 or lse.device != dev
-                                or not lse.is_contiguous()):
-            raise ValueError("lse must be contiguous float32 [R][Hq]")
+        if lse is not None:
+            if (lse.shape != (R, Hq) or lse.dtype is not torch.float32 or lse.get_device() != dev
+                    or not lse.is_contiguous()):
+                raise ValueError("lse must be contiguous float32 [R][Hq]")
+        elif want_lse:
+            lse = torch.empty((R, Hq), dtype=torch.float32, device=q.device)
         if ws is None:
-            ws = _workspace(decode_attention_workspace(cache, pages, Hq), dev)
-        st = lib().last_decode_attention(cache._struct, layer, pages._struct, Hq, float(scale), _ptr(q), q.stride(0),
-                                         _ptr(out), _ptr(lse), _ptr(ws), ws.numel() * ws.element_size(),
-                                         _stream(stream))
-        if st != LAST_OK:
-            raise LastError(st, "last_decode_attention")
-        return (out, lse) if lse is not None else out
+            ws = _workspace(decode_attention_workspace(cache, pages, Hq), q.device)
+        elif ws.get_device() != dev or not ws.is_contiguous():
+            raise ValueError("ws must be contiguous, on the cache's device")
+        st = lib().last_decode_attention(cache._at, layer, pages._at, Hq, scale, q.data_ptr(), rs, out.data_ptr(),
+                                         None if lse is None else lse.data_ptr(), ws.data_ptr(), ws.nbytes,
+                                         _raw_stream(dev, stream))
+    if st != LAST_OK:
+        raise LastError(st, "last_decode_attention")
+    return out if lse is None else (out, lse)
 
 
 def cache_prune(cache: Cache, src: Pages, dst: Pages, vis_start_h, cu_vis_h, kept: torch.Tensor, cu_keep_h,
                 vis_start=None, cu_vis=None, cu_keep=None, new_lens=None, stream=None) -> torch.Tensor:
     """last_cache_prune (Eq. 12 on a cache): the text and the kept visual tokens of every sequence, in every layer,
     from src's pages into dst's. The new lengths go to new_lens (dst.lens by default), which is returned."""
-    dev = cache.device
+    dev, device = cache._dev, cache.k.device
     with _on_device(dev, stream):
         R = src.R
         vs, cv, ck = (_host_i32(vis_start_h, "vis_start_h", (R,)), _host_i32(cu_vis_h, "cu_vis_h", (R + 1,)),
                       _host_i32(cu_keep_h, "cu_keep_h", (R + 1,)))
-        vis_start = _i32_dev(vs, dev) if vis_start is None else vis_start
-        cu_vis = _i32_dev(cv, dev) if cu_vis is None else cu_vis
-        cu_keep = _i32_dev(ck, dev) if cu_keep is None else cu_keep
+        vis_start = _i32_dev(vs, device) if vis_start is None else vis_start
+        cu_vis = _i32_dev(cv, device) if cu_vis is None else cu_vis
+        cu_keep = _i32_dev(ck, device) if cu_keep is None else cu_keep
         new_lens = dst.lens if new_lens is None else new_lens
-        for t, what, n in ((vis_start, "vis_start", R), (cu_vis, "cu_vis", R + 1), (cu_keep, "cu_keep", R + 1),
-                           (new_lens, "new_lens", R)):
-            _dev_i32(t, dev, what, (n,))
+        _dev_i32(vis_start, dev, "vis_start", (R,))
+        _dev_i32(cu_vis, dev, "cu_vis", (R + 1,))
+        _dev_i32(cu_keep, dev, "cu_keep", (R + 1,))
+        _dev_i32(new_lens, dev, "new_lens", (R,))
         _dev_i32(kept, dev, "kept")
-        if kept.numel() < int(ck[-1]) or src.table.device != dev or dst.table.device != dev:
+        if kept.numel() < int(ck[-1]) or src._dev != dev or dst._dev != dev:
             raise ValueError("kept must hold cu_keep's indices, and the page tables be on the cache's device")
-        st = lib().last_cache_prune(cache._struct, src._struct, dst._struct, _ptr(vis_start), _ptr(vs), _ptr(cu_vis),
-                                    _ptr(cv), _ptr(kept), _ptr(cu_keep), _ptr(ck), _ptr(new_lens), _stream(stream))
-        if st != LAST_OK:
-            raise LastError(st, "last_cache_prune")
-        return new_lens
+        st = lib().last_cache_prune(cache._at, src._at, dst._at, vis_start.data_ptr(), _ptr(vs), cu_vis.data_ptr(),
+                                    _ptr(cv), kept.data_ptr(), cu_keep.data_ptr(), _ptr(ck), new_lens.data_ptr(),
+                                    _raw_stream(dev, stream))
+    if st != LAST_OK:
+        raise LastError(st, "last_cache_prune")
+    return new_lens
 
 
 def cache_copy(cache: Cache, src_h, dst_h, src=None, dst=None, stream=None) -> None:
     """last_cache_copy: page src_h[i] copied to page dst_h[i], keys and values of every layer."""
-    dev = cache.device
+    dev, device = cache._dev, cache.k.device
     with _on_device(dev, stream):
         s = _host_i32(src_h, "src_h")
-        d = _host_i32(dst_h, "dst_h", s.shape)
         if s.ndim != 1:
             raise ValueError("src_h and dst_h must be one-dimensional")
-        src = _i32_dev(s, dev) if src is None else src
-        dst = _i32_dev(d, dev) if dst is None else dst
+        d = _host_i32(dst_h, "dst_h", s.shape)
+        src = _i32_dev(s, device) if src is None else src
+        dst = _i32_dev(d, device) if dst is None else dst
         _dev_i32(src, dev, "src", s.shape)
         _dev_i32(dst, dev, "dst", s.shape)
-        st = lib().last_cache_copy(cache._struct, len(s), _ptr(src), _ptr(s), _ptr(dst), _ptr(d), _stream(stream))
-        if st != LAST_OK:
-            raise LastError(st, "last_cache_copy")
+        st = lib().last_cache_copy(cache._at, len(s), src.data_ptr(), _ptr(s), dst.data_ptr(), _ptr(d), _raw_stream(dev, stream))
+    if st != LAST_OK:
+        raise LastError(st, "last_cache_copy")
 
 
 def budget(n: int, num: int, den: int) -> int:
