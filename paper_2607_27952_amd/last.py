@@ -540,7 +540,7 @@ def _host_i32(a, what: str, shape=None) -> np.ndarray:
     a = np.ascontiguousarray(a, dtype=np.int32)
     if shape is not None and a.shape != shape:
         raise ValueError(f"{what} must have the shape {tuple(shape)}")
-    return a
+    return a   # to a call as a.tobytes(): the copy of a short array costs less than asking numpy where it lies
 
 
 @dataclass(frozen=True, eq=False)
@@ -637,13 +637,19 @@ class Rotary:
 
 def _rows(t: torch.Tensor, dev: int, dtype, G: int, T: int, H, D: int, what: str):
     """t [G][T][H][D] (H None: any) as the three numbers of a last_heads, and its heads."""
-    if t.dim() != 4 or t.dtype is not dtype or t.get_device() != dev:
+    if t.dtype is not dtype or t.get_device() != dev or t.dim() != 4:
         raise ValueError(f"{what} must be [G][T][heads][Dh], of the dtype and on the device of the call")
     g, n, h, d = t.shape
     ls, ts, hs, es = t.stride()
-    if g != G or n != T or d != D or (H is not None and h != H) or es != 1 or (h > 1 and hs != D):
+    if g != G or n != T or d != D or (h != H and H is not None) or es != 1 or (hs != D and h > 1):
         raise ValueError(f"{what} must be [{G}][{T}][{'heads' if H is None else H}][{D}] with contiguous heads")
     return (t.data_ptr(), ls, ts), h
+
+
+def _rows_like(t: torch.Tensor, T: int, H: int, D: int):
+    """A new contiguous tensor of t's shape, and its last_heads."""
+    out = torch.empty_like(t, memory_format=torch.contiguous_format)
+    return out, (out.data_ptr(), T * H * D, H * D)
 
 
 _FourHeads = ctypes.c_int64 * 12   # four last_heads
@@ -678,12 +684,14 @@ def rotary(rot: Rotary, pos: torch.Tensor, q: Optional[torch.Tensor], k: Optiona
                 continue
             r, h = _rows(t, dev, dtype, G, T, None, D, what)
             if out is None:
-                out = torch.empty((G, T, h, D), dtype=dtype, device=t.device)
+                out, ro = _rows_like(t, T, h, D)
                 if what == "q":
                     q_out = out
                 else:
                     k_out = out
-            rows += [r, _rows(out, dev, dtype, G, T, h, D, what + "_out")[0]]
+            else:
+                ro = _rows(out, dev, dtype, G, T, h, D, what + "_out")[0]
+            rows += [r, ro]
             heads.append(h)
         h4 = _FourHeads(*rows[0], *rows[1], *rows[2], *rows[3])
         p = ctypes.addressof(h4)
@@ -712,8 +720,9 @@ def rotary_append(rot: Optional[Rotary], cache: Cache, pages: Pages, pos: Option
         if q is not None:
             qr, Hq = _rows(q, dev, dtype, G, T, None, D, "q")
             if q_out is None:
-                q_out = torch.empty((G, T, Hq, D), dtype=dtype, device=q.device)
-            qo, _ = _rows(q_out, dev, dtype, G, T, Hq, D, "q_out")
+                q_out, qo = _rows_like(q, T, Hq, D)
+            else:
+                qo, _ = _rows(q_out, dev, dtype, G, T, Hq, D, "q_out")
         if rot is not None:
             if pos is None:
                 raise ValueError("a rotation needs positions")
@@ -729,7 +738,8 @@ def rotary_append(rot: Optional[Rotary], cache: Cache, pages: Pages, pos: Option
         h4 = _FourHeads(*qr, *qo, *kr, *vr)
         p = ctypes.addressof(h4)
         st = lib().last_rotary_append(rot._at[0] if rot is not None else None, cache._at, layer, G, pages._at, T,
-                                      _ptr(cu_new), _ptr(cu), Hq, at, p, p + 24, p + 48, p + 72, _raw_stream(dev, stream))
+                                      None if cu is None else cu_new.data_ptr(), None if cu is None else cu.tobytes(),
+                                      Hq, at, p, p + 24, p + 48, p + 72, _raw_stream(dev, stream))
     if st != LAST_OK:
         raise LastError(st, "last_rotary_append")
     return q_out
@@ -752,7 +762,7 @@ def decode_attention(cache: Cache, pages: Pages, q: torch.Tensor, layer: int = 0
         if R != pages.R or d != D or es != 1 or (Hq > 1 and hs != D):
             raise ValueError("q must have a row of contiguous heads for every sequence")
         if out is None:
-            out = torch.empty((R, Hq, D), dtype=dtype, device=q.device)
+            out = torch.empty_like(q, memory_format=torch.contiguous_format)
         elif out.shape != q.shape or out.dtype is not dtype or out.get_device() != dev or not out.is_contiguous():
             raise ValueError("out must be contiguous, with q's shape and dtype")
         if lse is not None:
@@ -793,8 +803,8 @@ def cache_prune(cache: Cache, src: Pages, dst: Pages, vis_start_h, cu_vis_h, kep
         _dev_i32(kept, dev, "kept")
         if kept.numel() < int(ck[-1]) or src._dev != dev or dst._dev != dev:
             raise ValueError("kept must hold cu_keep's indices, and the page tables be on the cache's device")
-        st = lib().last_cache_prune(cache._at, src._at, dst._at, vis_start.data_ptr(), _ptr(vs), cu_vis.data_ptr(),
-                                    _ptr(cv), kept.data_ptr(), cu_keep.data_ptr(), _ptr(ck), new_lens.data_ptr(),
+        st = lib().last_cache_prune(cache._at, src._at, dst._at, vis_start.data_ptr(), vs.tobytes(), cu_vis.data_ptr(),
+                                    cv.tobytes(), kept.data_ptr(), cu_keep.data_ptr(), ck.tobytes(), new_lens.data_ptr(),
                                     _raw_stream(dev, stream))
     if st != LAST_OK:
         raise LastError(st, "last_cache_prune")
@@ -813,7 +823,7 @@ def cache_copy(cache: Cache, src_h, dst_h, src=None, dst=None, stream=None) -> N
         dst = _i32_dev(d, device) if dst is None else dst
         _dev_i32(src, dev, "src", s.shape)
         _dev_i32(dst, dev, "dst", s.shape)
-        st = lib().last_cache_copy(cache._at, len(s), src.data_ptr(), _ptr(s), dst.data_ptr(), _ptr(d), _raw_stream(dev, stream))
+        st = lib().last_cache_copy(cache._at, len(s), src.data_ptr(), s.tobytes(), dst.data_ptr(), d.tobytes(), _raw_stream(dev, stream))
     if st != LAST_OK:
         raise LastError(st, "last_cache_copy")
 
