@@ -1,10 +1,14 @@
 // Pages of a cache: whole pages copied, and a prompt's cache compacted to its
 // text and kept visual tokens (Sec. 3.4, Eq. 12 on the cache). Both move rows
 // of Dh elements, 16 bytes a thread, between pages of one pool; the host has
-// checked that no row written is one that is read. The memory bounds both:
-// 1024 pages of 64 tokens and 8 heads in 2 layers, 1.07 GB moved, take 184 us
-// (5.8 TB/s); compacting keeps single rows of 256 bytes and reaches 4.2 to 4.7.
-// One piece a thread and many blocks: four pieces a thread took 207 us.
+// checked that no row written is one that is read. The memory bounds both.
+//
+// Copy: a piece a thread, many blocks, one pool after the other. 1024 pages of
+// 64 tokens and 8 heads in 2 layers, 1.07 GB moved, take 179 us (6.0 TB/s; four
+// pieces a thread 207); 2000 pages of 16 tokens and 4 heads in 4 layers 102
+// (109 with the layers of a page one after the other).
+// Prune keeps single rows of 128 to 512 bytes: 64 sequences of 640 tokens to
+// 128, 2 layers of 32 heads, 537 MB moved, 107 us (5.0 TB/s).
 #include <algorithm>
 
 #include "last_internal.h"
@@ -15,6 +19,7 @@ using last::CopyArgs;
 using last::PruneArgs;
 
 constexpr int kRowsPrune = 32;   // most new tokens of a block
+constexpr int kItems = 4;        // 16-byte pieces of a thread
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 // Piece i of a tile of `inner` x `outer` rows of `1 << lc` pieces, as its
@@ -31,10 +36,9 @@ __global__ __launch_bounds__(256) void k_cache_copy(CopyArgs a) {
   int64_t b = blockIdx.x;
   const int chunk = (int)(b % a.chunks);
   b /= a.chunks;
-  const int kv = (int)(b & 1);
-  b >>= 1;
-  const int g = (int)(b % a.G);
-  const int64_t i = b / a.G;
+  const int64_t i = b % a.n;   // one pool after the other: they share no translations
+  b /= a.n;
+  const int kv = (int)(b & 1), g = (int)(b >> 1);
   const int32_t from = a.src[i], to = a.dst[i];
   if ((uint32_t)from >= (uint32_t)a.n_pages || (uint32_t)to >= (uint32_t)a.n_pages) return;
   u32x4 *base = (u32x4 *)(kv ? a.v : a.k) + g * a.layer_stride;
@@ -88,20 +92,30 @@ __global__ __launch_bounds__(256) void k_cache_prune(PruneArgs a) {
     to[threadIdx.x] = d;
   }
   __syncthreads();
-  // rows in the order they lie in: heads of a token, or tokens of a head
+  // Rows in the order they lie in: heads of a token, or tokens of a head. All
+  // of a thread's loads are issued before its first store: loads and stores
+  // count together, so a load behind a store would wait for that too.
   const uint32_t inner = a.heads_inner ? a.Hkv : a.rows;
-  const uint32_t pieces = ((uint32_t)a.Hkv * a.rows) << a.lc;
-  for (uint32_t p = threadIdx.x; p < pieces; p += 256) {
-    const Cell e = cell(p, a.lc, inner);
-    const int head = a.heads_inner ? e.inner : e.outer, t = a.heads_inner ? e.outer : e.inner;
-    if (to[t] < 0) continue;
-    const bool zero = from[t] < 0;
-    const int64_t off = e.c + head * a.head_stride, src = off + (zero ? 0 : from[t]), dst = off + to[t];
-    for (int c = first; c < last; ++c) {
-      u32x4 *base = (u32x4 *)(c & 1 ? a.v : a.k) + (c >> 1) * a.layer_stride;
-      const u32x4 x = base[src];   // a row of the cache, also where it is not used
-      __builtin_nontemporal_store(zero ? u32x4{} : x, base + dst);
+  const uint32_t pieces = ((uint32_t)a.Hkv * a.rows) << a.lc, total = pieces * (last - first);
+  for (uint32_t u0 = 0; u0 < total; u0 += 256 * kItems) {
+    u32x4 x[kItems];
+    u32x4 *dst[kItems];
+#pragma unroll
+    for (int j = 0; j < kItems; ++j) {
+      dst[j] = nullptr;
+      if (u0 + j * 256 >= total) continue;   // the whole block has no more
+      const uint32_t u = min(u0 + j * 256 + threadIdx.x, total - 1), o = u / pieces;
+      const Cell e = cell(u - o * pieces, a.lc, inner);
+      const int head = a.heads_inner ? e.inner : e.outer, t = a.heads_inner ? e.outer : e.inner, c = first + o;
+      u32x4 *base = (u32x4 *)(c & 1 ? a.v : a.k) + (c >> 1) * a.layer_stride + e.c + head * a.head_stride;
+      const int64_t f = from[t], d = to[t];
+      if (d >= 0 && u0 + j * 256 + threadIdx.x < total) dst[j] = base + d;
+      x[j] = u32x4{};
+      if (dst[j] && f >= 0) x[j] = base[f];
     }
+#pragma unroll
+    for (int j = 0; j < kItems; ++j)
+      if (dst[j]) __builtin_nontemporal_store(x[j], dst[j]);
   }
 }
 
@@ -120,19 +134,19 @@ hipError_t launch_cache_copy(const CopyArgs &a, int64_t blocks, hipStream_t s) {
   return launch_end(s);
 }
 
-// A block moves as many tokens as give its threads a piece each (4 at least),
-// in as many layers' keys and values as leave 4 blocks a compute unit: what it
-// looks up (where each token comes from and goes to) then serves all of them.
-// Eight sequences of 16384 visual tokens to 1024, 4 layers of 4 heads: all in a
-// block 33 us, one each 40; 32 sequences of 288 to 16384 to a ninth, 4 layers
-// of 2 heads: all 26, one each 53. Eight of 300 to 600, where all would leave
-// 1 block a unit: two or four pools a block 5.3, all 5.7.
+// A block moves as many tokens as give its threads a piece each (2 at least,
+// for 32 heads: 107 us against 112 with 4 and 110 with 1), in so many layers'
+// keys and values that a thread has up to kItems pieces, if that leaves 4
+// blocks a compute unit: what it looks up (where each token comes from and
+// goes to) then serves all of them. Eight sequences of 16384 visual tokens to
+// 1024, 4 layers of 4 heads: 32 us, one pool a block 40; 32 sequences of 288 to
+// 16384 to a ninth, 4 layers of 2 heads: 26, one pool a block 53.
 int64_t prune_blocks(PruneArgs *a) {
-  a->rows = std::max(4, std::min(kRowsPrune, 256 / std::min(256, a->Hkv << a->lc)));
+  a->rows = std::max(2, std::min(kRowsPrune, 256 / std::min(256, a->Hkv << a->lc)));
   a->tiles = std::max(1, (a->max_new + a->rows - 1) / a->rows);
   const int pools = 2 * a->G;
   const int64_t all = (int64_t)a->R * pools * a->tiles;
-  a->span = (int32_t)std::max<int64_t>(1, std::min<int64_t>(pools, all / (4 * device_cus())));
+  a->span = (int32_t)std::max<int64_t>(1, std::min<int64_t>({pools, 256 * kItems / ((a->Hkv * a->rows) << a->lc), all / (4 * device_cus())}));
   return (int64_t)a->R * a->tiles * ((pools + a->span - 1) / a->span);
 }
 
