@@ -1,0 +1,138 @@
+"""The cache's calls where they change how they lay their work out (needs an MI355X): batches past a wave of
+sequences, blocks that serve several sequences, heads beside each other, several tokens, layers or batches of
+rows a block. Bounds as in cache_ref.py."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import cache_ref as ref
+from paper_2607_27952_amd import last
+from test_gpu_cache import BF, F32, decode_case, freqs, gen, same_bits, up, within
+
+pytestmark = pytest.mark.gpu
+
+
+def check(cache, pages, q, exp, lens, layer):
+    out, lse, ob, lb = exp
+    got, got_lse = last.decode_attention(cache, pages, q.cuda(), layer=layer, want_lse=True)
+    within(got, out, ob, "out")
+    some = np.asarray(lens) > 0
+    within(got_lse[some], lse[some], lb[some], "lse")
+    assert bool((got_lse[~torch.from_numpy(some)] == -math.inf).all()) and bool((got[~torch.from_numpy(some)] == 0).all())
+    again, again_lse = last.decode_attention(cache, pages, q.cuda(), layer=layer, want_lse=True)
+    assert same_bits(again, got) and same_bits(again_lse, got_lse)
+
+
+@pytest.mark.parametrize("dtype,Dh,Hq,Hkv,ps,major", [
+    (BF, 128, 4, 2, 16, True), (BF, 128, 3, 3, 32, True), (BF, 64, 36, 2, 8, True), (F32, 64, 8, 8, 16, True),
+    (BF, 128, 14, 2, 64, False), (F32, 128, 20, 1, 256, False)])
+@pytest.mark.parametrize("R,longest", [(150, 900), (67, 4000), (3, 9000)])
+def test_decode_batches(dtype, Dh, Hq, Hkv, ps, major, R, longest):
+    """Many sequences of very different lengths, empty ones between them: stretches of the line that end, begin
+    and lie inside units, and units of one part, two and many."""
+    r = np.random.default_rng(R + Dh)
+    lens = np.exp(r.uniform(0, math.log(longest), R)).astype(int)
+    lens[r.random(R) < 0.15] = 0
+    lens[-1 if R > 100 else 0] = longest
+    cache, pages, q, exp = decode_case(R, dtype, Dh, Hq, Hkv, ps, tuple(int(n) for n in lens), major, G=1, layer=0)
+    check(cache, pages, q, exp, lens, 0)
+
+
+@pytest.mark.parametrize("lens", [(0,) * 70, (1,) + (0,) * 69, (0,) * 69 + (200,), (3, 0) * 35])
+@pytest.mark.parametrize("major", [False, True])
+def test_decode_far_below_the_bounds(lens, major):
+    """A call laid out for long sequences whose lengths on the device are short: fewer steps than blocks."""
+    R, ps, Hkv, Dh = len(lens), 16, 2, 128
+    gg = gen(3)
+    table = np.tile(np.arange(128, dtype=np.int32), (R, 1))      # sequences may share pages
+    kp, vp = (ref.pool(gg, 1, 128, Hkv, ps, Dh, BF, major) for _ in "kv")
+    q = torch.randn((R, 12, Dh), generator=gg).to(BF)
+    pages = last.Pages(lens_h=np.asarray([2048] * 20 + [300] * (R - 20)), table=torch.from_numpy(table).cuda(),
+                       lens=torch.tensor(lens, dtype=torch.int32).cuda())
+    check(last.Cache(up(kp), up(vp)), pages, q, ref.decode(q, kp[0], vp[0], table, lens), lens, 0)
+
+
+def test_decode_shared_workspace_of_unlike_calls():
+    """One workspace for calls of unlike shapes one after the other, full of NaN at first."""
+    cases = [decode_case(41, BF, 128, 28, 4, 16, (3000, 40, 0), G=1, layer=0),
+             decode_case(42, BF, 64, 12, 2, 8, (1, 1999), True, G=1, layer=0),
+             decode_case(43, F32, 128, 6, 2, 32, (777,), True, G=1, layer=0)]
+    need = max(last.decode_attention_workspace(c[0], c[1], c[2].shape[1]) for c in cases)
+    ws = torch.full((need // 4,), math.nan, device="cuda")
+    for cache, pages, q, (out, _, ob, _) in cases + cases[::-1]:
+        within(last.decode_attention(cache, pages, q.cuda(), ws=ws), out, ob)
+
+
+@pytest.mark.parametrize("dtype,Dh,Hq,Hkv,ps,major,adjacent", [(BF, 64, 3, 1, 16, False, False), (F32, 64, 2, 2, 8, True, True),
+                                                               (BF, 128, 12, 2, 128, False, False), (BF, 128, 40, 40, 16, True, False)])
+def test_append_many_tokens(dtype, Dh, Hq, Hkv, ps, major, adjacent):
+    """Ragged prompts of so many tokens that a block takes several, whose groups straddle sequences."""
+    new = (1, 2500, 3, 0, 1, 1700, 2)
+    gg, rng = gen(17), np.random.default_rng(17)
+    T, F = sum(new), Dh // 2
+    table, pages = ref.table_for(rng, new, ps)
+    kp, vp = (ref.pool(gg, 1, pages, Hkv, ps, Dh, dtype, major) for _ in "kv")
+    cache = last.Cache(up(kp), up(vp))
+    pos = torch.randint(0, 60000, (2, T), generator=gg, dtype=torch.int32)
+    axis = np.arange(F) % 2
+    rot = last.Rotary.make(freqs(F), axis=axis, adjacent=adjacent)
+    q, k, v = (torch.randn((1, T, h, Dh), generator=gg).to(dtype) for h in (Hq, Hkv, Hkv))
+    cu = np.concatenate([[0], np.cumsum(new)])
+    got = last.rotary_append(rot, cache, last.Pages.make(table, new), pos.cuda(), q.cuda(), k.cuda(), v.cuda(), cu_new_h=cu)
+    e = ref.rotary(q, pos, freqs(F), axis, adjacent)
+    within(got, e, ref.rotary_bound(q, e, F, adjacent), "q")
+    e = ref.rotary(k, pos, freqs(F), axis, adjacent)
+    b = ref.rotary_bound(k, e, F, adjacent)
+    exp_k, exp_v, tol = kp.double(), vp.clone(), torch.zeros(kp.shape, dtype=torch.float64)
+    for r, n in enumerate(new):
+        at = np.arange(n)
+        page, slot = torch.from_numpy(table[r, at // ps].astype(np.int64)), torch.from_numpy(at % ps)
+        rows = slice(int(cu[r]), int(cu[r + 1]))
+        exp_k[0, page, :, slot], tol[0, page, :, slot], exp_v[0, page, :, slot] = e[0, rows], b[0, rows], v[0, rows]
+    within(cache.k, exp_k, tol, "keys")
+    assert same_bits(cache.v.cpu(), exp_v)
+
+
+@pytest.mark.parametrize("dtype,Dh,Hkv,ps,major,G,R", [
+    (BF, 128, 4, 16, False, 4, 9), (BF, 128, 2, 8, True, 3, 20), (F32, 128, 33, 16, False, 1, 3), (BF, 64, 1, 32, False, 5, 40),
+    (F32, 64, 16, 64, True, 2, 6)])
+def test_prune_batches(dtype, Dh, Hkv, ps, major, G, R):
+    """So many rows that a block takes several layers, and heads so wide that it takes several turns."""
+    gg, rng = gen(R), np.random.default_rng(R)
+    N = rng.integers(1, 900, R)
+    K = np.minimum(N, rng.integers(0, 400, R))
+    vis, tail = rng.integers(0, 50, R), rng.integers(0, 60, R)
+    lens, after = [int(x) for x in N + vis + tail], [int(x) for x in K + vis + tail]
+    table, pages = ref.table_for(rng, lens + after, ps)
+    src, dst = np.ascontiguousarray(table[:R]), np.ascontiguousarray(table[R:])
+    kp, vp = (ref.pool(gg, G, pages, Hkv, ps, Dh, dtype, major) for _ in "kv")
+    kept = [np.sort(rng.choice(n, k, replace=False)) for n, k in zip(N, K)]
+    cu_vis, cu_keep = (np.concatenate([[0], np.cumsum(x)]) for x in (N, K))
+    cache = last.Cache(up(kp), up(vp))
+    flat = torch.from_numpy(np.concatenate(kept).astype(np.int32)).cuda()
+    got = last.cache_prune(cache, last.Pages.make(src, lens), last.Pages.make(dst, after), vis, cu_vis, flat, cu_keep)
+    assert got.tolist() == after
+    for p, x in ((kp, cache.k), (vp, cache.v)):
+        e = p.clone()
+        for r in range(R):
+            old = ref.prune_index(lens[r], int(vis[r]), int(N[r]), kept[r])
+            i = np.arange(len(old))
+            a, b, c, d = (torch.from_numpy(y.astype(np.int64)) for y in (src[r, old // ps], old % ps, dst[r, i // ps], i % ps))
+            e[:, c, :, d] = p[:, a, :, b]
+        assert same_bits(x.cpu(), e)
+
+
+@pytest.mark.parametrize("dtype,Dh,Hkv,ps,major,G,n", [(BF, 128, 7, 16, False, 2, 301), (F32, 64, 2, 1024, True, 1, 20),
+                                                       (BF, 64, 1, 8, False, 3, 1000)])
+def test_copy_batches(dtype, Dh, Hkv, ps, major, G, n):
+    gg, rng = gen(n), np.random.default_rng(n)
+    kp, vp = (ref.pool(gg, G, 2 * n + 1, Hkv, ps, Dh, dtype, major) for _ in "kv")
+    ids = rng.permutation(2 * n + 1)
+    cache = last.Cache(up(kp), up(vp))
+    last.cache_copy(cache, ids[:n], ids[n:2 * n])
+    for p, got in ((kp, cache.k), (vp, cache.v)):
+        e = p.clone()
+        e[:, ids[n:2 * n]] = p[:, ids[:n]]
+        assert same_bits(got.cpu(), e)
