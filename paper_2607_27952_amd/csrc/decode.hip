@@ -187,6 +187,20 @@ struct Share {
     return step < head ? step / (each + 1) : more + (step - head) / each;
   }
 };
+// Inclusive sums over a wave, whose sum is returned in `sum`: DPP shifts inside
+// rows of 16 lanes (a tenth of the time of shuffles, which pass through LDS and
+// would stand before a block's first load), then the rows' ends.
+__device__ __forceinline__ int wave_scan(int v, int *sum) {
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, true);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, true);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, true);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, true);
+  const int a = __builtin_amdgcn_readlane(v, 15), b = a + __builtin_amdgcn_readlane(v, 31);
+  const int c = b + __builtin_amdgcn_readlane(v, 47), row = (threadIdx.x & 63) >> 4;
+  *sum = c + __builtin_amdgcn_readlane(v, 63);
+  return v + (row == 0 ? 0 : row == 1 ? a : row == 2 ? b : c);
+}
+
 // Where a block's stretch begins: its sequence, the line's steps before that
 // sequence, and the line's length. Called by whole waves.
 struct Start {
@@ -196,26 +210,25 @@ template <int STEP>
 __device__ __forceinline__ Start find_start(const DecodeArgs &a, int units, int block) {
   const int lane = threadIdx.x & 63;
   auto steps = [&](int r) { return r < a.R ? units * ((clamp_len(a, r) + STEP - 1) / STEP) : 0; };
-  int n = steps(lane), total = n;   // of the first 64 sequences, which are often all
-  for (int r = 64 + lane; r < a.R; r += 64) total += steps(r);
-#pragma unroll
-  for (int o = 32; o; o >>= 1) total += __shfl_xor(total, o);
+  int n = steps(lane), sum, total;   // of the first 64 sequences, which are often all
+  int x = wave_scan(n, &sum);
+  total = sum;
+  if (a.R > 64) {
+    int rest = 0, more;
+    for (int r = 64 + lane; r < a.R; r += 64) rest += steps(r);
+    wave_scan(rest, &more);
+    total += more;
+  }
   const int at = Share(total, a.blocks).start(block);
   int base = 0;
   for (int r0 = 0; r0 < a.R; r0 += 64) {
-    if (r0) n = steps(r0 + lane);
-    int x = n;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const int y = __shfl_up(x, o);
-      if (lane >= o) x += y;
-    }
+    if (r0) x = wave_scan(n = steps(r0 + lane), &sum);
     const unsigned long long behind = __ballot(base + x > at);
     if (behind) {
       const int l = __ffsll((long long)behind) - 1;
       return Start{r0 + l, base + __builtin_amdgcn_readlane(x - n, l), total};
     }
-    base += __builtin_amdgcn_readlane(x, 63);
+    base += sum;
   }
   return Start{a.R, base, total};   // behind the line's end
 }

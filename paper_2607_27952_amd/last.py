@@ -676,27 +676,24 @@ def rotary(rot: Rotary, pos: torch.Tensor, q: Optional[torch.Tensor], k: Optiona
         code = _dtype_code(x)
         G, T, _, D = x.shape
         at = _positions(pos, rot, T, dev)
-        rows, heads = [], []
-        for t, out, what in ((q, q_out, "q"), (k, k_out, "k")):
-            if t is None:
-                rows += [_NO_HEADS, _NO_HEADS]
-                heads.append(0)
-                continue
-            r, h = _rows(t, dev, dtype, G, T, None, D, what)
-            if out is None:
-                out, ro = _rows_like(t, T, h, D)
-                if what == "q":
-                    q_out = out
-                else:
-                    k_out = out
+        qr = qo = kr = ko = _NO_HEADS
+        Hq = Hkv = 0
+        if q is not None:
+            qr, Hq = _rows(q, dev, dtype, G, T, None, D, "q")
+            if q_out is None:
+                q_out, qo = _rows_like(q, T, Hq, D)
             else:
-                ro = _rows(out, dev, dtype, G, T, h, D, what + "_out")[0]
-            rows += [r, ro]
-            heads.append(h)
-        h4 = _FourHeads(*rows[0], *rows[1], *rows[2], *rows[3])
+                qo, _ = _rows(q_out, dev, dtype, G, T, Hq, D, "q_out")
+        if k is not None:
+            kr, Hkv = _rows(k, dev, dtype, G, T, None, D, "k")
+            if k_out is None:
+                k_out, ko = _rows_like(k, T, Hkv, D)
+            else:
+                ko, _ = _rows(k_out, dev, dtype, G, T, Hkv, D, "k_out")
+        h4 = _FourHeads(*qr, *kr, *qo, *ko)
         p = ctypes.addressof(h4)
-        st = lib().last_rotary(rot._at[1 if inverse else 0], code, G, T, heads[0], heads[1], D, at, p, p + 48, p + 24,
-                               p + 72, _raw_stream(dev, stream))
+        st = lib().last_rotary(rot._at[1 if inverse else 0], code, G, T, Hq, Hkv, D, at, p, p + 24, p + 48, p + 72,
+                               _raw_stream(dev, stream))
     if st != LAST_OK:
         raise LastError(st, "last_rotary")
     return q_out if q is not None else None, k_out if k is not None else None
@@ -770,7 +767,7 @@ def decode_attention(cache: Cache, pages: Pages, q: torch.Tensor, layer: int = 0
                     or not lse.is_contiguous()):
                 raise ValueError("lse must be contiguous float32 [R][Hq]")
         elif want_lse:
-            lse = torch.empty((R, Hq), dtype=torch.float32, device=q.device)
+            lse = q.new_empty((R, Hq), dtype=torch.float32)
         if ws is None:
             ws = _workspace(decode_attention_workspace(cache, pages, Hq), q.device)
         elif ws.get_device() != dev or not ws.is_contiguous():
