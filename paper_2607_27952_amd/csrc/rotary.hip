@@ -169,7 +169,7 @@ __global__ __launch_bounds__(256) void k_rotary(RotaryArgs a) {
         y[e] = w;
       }
     }
-    // Past the caches where the rows go to pages (appending 123000 tokens of
+    // Past the caches where the rows go to pages (appending 108000 tokens of
     // 12 + 2 heads 154 against 160 us), not where they stay rows (132096 tokens
     // of 28 + 4 heads 354 against 363).
     vec *d0 = reinterpret_cast<vec *>(dst + p0 * VEC), *d1 = reinterpret_cast<vec *>(dst + p1 * VEC);
@@ -204,7 +204,7 @@ namespace last {
 // several blocks until there are about 2 a compute unit. In bf16, heads of 128:
 //   132096 tokens, 28 + 4 heads     1 token 363 us, 2 380, 4 398
 //   100000 tokens, 12 + 2 heads     1 token 180 us, 2 134, 4 160
-//   appending 123000, 12 + 2 + 2    1 token 304 us, 2 190, 4 154, 8 164
+//   appending 108000, 12 + 2 + 2    1 token 304 us, 2 190, 4 154, 8 164
 //   appending 16384, 28 + 4 + 4     1 token  68 us, 2  59, 4  61
 static void shape(RotaryArgs *a, int items, bool append, int cus, int64_t *blocks) {
   const int heads = a->Hq + (append ? 2 : 1) * a->Hkv;
