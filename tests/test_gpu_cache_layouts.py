@@ -136,3 +136,100 @@ def test_copy_batches(dtype, Dh, Hkv, ps, major, G, n):
         e = p.clone()
         e[:, ids[n:2 * n]] = p[:, ids[:n]]
         assert same_bits(got.cpu(), e)
+
+
+def test_nothing_to_do():
+    """No tokens, no pages: nothing is launched, and nothing of the cache changes."""
+    gg = gen(1)
+    kp, vp = (ref.pool(gg, 2, 4, 2, 16, 64, BF) for _ in "kv")
+    cache = last.Cache(kp.cuda(), vp.cuda())
+    rot = last.Rotary.make(freqs(32))
+    none = torch.empty((2, 0, 2, 64), dtype=BF, device="cuda")
+    pos = torch.empty((1, 0), dtype=torch.int32, device="cuda")
+    q, k = last.rotary(rot, pos, none, none)
+    assert q.shape == k.shape == none.shape
+    seqs = last.Pages.make([[0, 1], [2, 3]], [20, 0])
+    assert last.rotary_append(rot, cache, seqs, pos, none, none, none, cu_new_h=[0, 0, 0]).shape == none.shape
+    last.cache_copy(cache, [], [])
+    empty = last.Pages.make([[0, 1], [2, 3]], [0, 0])
+    got = last.cache_prune(cache, empty, last.Pages.make([[3], [2]], [0, 5]), [0, 0], [0, 0, 0],
+                           torch.empty(0, dtype=torch.int32, device="cuda"), [0, 0, 0])
+    assert got.tolist() == [0, 0]
+    assert same_bits(cache.k.cpu(), kp) and same_bits(cache.v.cpu(), vp)
+
+
+def test_prune_takes_any_indices():
+    """Kept indices repeated and out of order are copied as they stand."""
+    gg, ps = gen(2), 16
+    kp, vp = (ref.pool(gg, 1, 12, 2, ps, 128, BF) for _ in "kv")
+    cache = last.Cache(kp.cuda(), vp.cuda())
+    src, dst = np.asarray([[7, 1, 4, 0]], np.int32), np.asarray([[9, 8]], np.int32)
+    kept = np.asarray([30, 3, 3, 0, 39, 30, 30], np.int32)
+    last.cache_prune(cache, last.Pages.make(src, [55]), last.Pages.make(dst, [22]), [5], [0, 40],
+                     torch.from_numpy(kept).cuda(), [0, 7])
+    old = [ref.prune_index(55, 5, 40, kept)]
+    for p, x in ((kp, cache.k), (vp, cache.v)):
+        assert same_bits(x.cpu(), ref.prune(p, src, dst, ps, old))
+
+
+def test_two_calls_at_once():
+    """Split calls on two streams, each with its own workspace, while a third stream copies pages of the cache."""
+    lens = ((5000, 3, 800), (2000, 2000, 1))
+    cases = [decode_case(51 + i, BF, 128, 28, 4, 16, n, G=1, layer=0) for i, n in enumerate(lens)]
+    streams = [torch.cuda.Stream() for _ in range(3)]
+    qs = [c[2].cuda() for c in cases]
+    used = set(cases[0][1].table_h[cases[0][1].table_h < 2 ** 30].tolist())
+    free = [p for p in range(cases[0][0].k.shape[1]) if p not in used]
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(4):
+        last.cache_copy(cases[0][0], [int(cases[0][1].table_h[0, 0])], free[:1], stream=streams[2])
+        for i, (c, q) in enumerate(zip(cases, qs)):
+            got[i].append(last.decode_attention(c[0], c[1], q, stream=streams[i]))
+    torch.cuda.synchronize()
+    for (_, _, _, (out, _, ob, _)), g in zip(cases, got):
+        for x in g:
+            within(x, out, ob)
+            assert same_bits(x, g[0])
+
+
+def test_captured_prune_and_copy():
+    """Prune and copy captured once and replayed on other contents, indices and lengths' targets, with eager work
+    between the replays, equal the plain forms every time."""
+    gg, rng, ps, G = gen(61), np.random.default_rng(61), 16, 2
+    lens, vis, N, K = (200, 90), (7, 30), (150, 40), (33, 12)
+    after = [n - a + b for n, a, b in zip(lens, N, K)]
+    table, pages = ref.table_for(rng, list(lens) + after, ps)
+    src, dst = np.ascontiguousarray(table[:2]), np.ascontiguousarray(table[2:])
+    cu_vis, cu_keep = (np.concatenate([[0], np.cumsum(x)]).astype(np.int32) for x in (N, K))
+    kd, vd = (torch.zeros((G, pages + 2, 2, ps, 128), dtype=BF, device="cuda") for _ in "kv")
+    cache, full, into = last.Cache(kd, vd), last.Pages.make(src, lens), last.Pages.make(dst, after)
+    kept = torch.zeros(sum(K), dtype=torch.int32, device="cuda")
+    dev = [torch.from_numpy(np.asarray(x, np.int32)).cuda() for x in (vis, cu_vis, cu_keep, [src[0, 0], dst[1, 0]], [pages, pages + 1])]
+
+    def step():
+        last.cache_prune(cache, full, into, vis, cu_vis, kept, cu_keep, vis_start=dev[0], cu_vis=dev[1], cu_keep=dev[2])
+        last.cache_copy(cache, [src[0, 0], dst[1, 0]], [pages, pages + 1], src=dev[3], dst=dev[4])
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for _ in range(4):
+        kp, vp = (ref.pool(gg, G, pages + 2, 2, ps, 128, BF) for _ in "kv")
+        kd.copy_(kp), vd.copy_(vp)
+        ids = [np.sort(rng.choice(n, k, replace=False)) for n, k in zip(N, K)]
+        kept.copy_(torch.from_numpy(np.concatenate(ids).astype(np.int32)))
+        into.lens.fill_(-1)
+        torch.cuda.synchronize()
+        graph.replay()
+        assert into.lens.tolist() == after
+        old = [ref.prune_index(lens[r], vis[r], N[r], ids[r]) for r in range(2)]
+        for p, x in ((kp, kd), (vp, vd)):
+            e = ref.prune(p, src, dst, ps, old)
+            e[:, pages], e[:, pages + 1] = e[:, src[0, 0]], e[:, dst[1, 0]]
+            assert same_bits(x.cpu(), e)
