@@ -812,20 +812,24 @@ last_status last_cache_prune(const last_cache *c, const last_pages *src, const l
     a.max_new = std::max(a.max_new, len - n + k);
   }
   {   // no page written may be read, or be written twice
-    PageSet read(c->n_pages), written(c->n_pages);
-    if (!read.ok() || !written.ok()) return LAST_ERR_UNSUPPORTED;
-    for (int32_t r = 0; r < R; ++r)
-      for (int32_t i = 0; i < (src->lens_h[r] + ps - 1) / ps; ++i)
-        read.add(src->table_h[(int64_t)r * src->max_pages + i]);
+    PageSet written(c->n_pages);
+    if (!written.ok()) return LAST_ERR_UNSUPPORTED;
     for (int32_t r = 0; r < R; ++r) {
       const int32_t m = src->lens_h[r] - (cu_vis_h[r + 1] - cu_vis_h[r]) + (cu_keep_h[r + 1] - cu_keep_h[r]);
+      const int32_t *from = src->table_h + (int64_t)r * src->max_pages, *to = dst->table_h + (int64_t)r * dst->max_pages;
       for (int32_t i = 0; i < (m + ps - 1) / ps; ++i) {
-        const int32_t to = dst->table_h[(int64_t)r * dst->max_pages + i];
-        if ((int64_t)(i + 1) * ps <= vis_start_h[r] && to == src->table_h[(int64_t)r * src->max_pages + i]) continue;
-        if (read.has(to) || written.has(to)) return LAST_ERR_INVALID;
-        written.add(to);
+        if ((int64_t)(i + 1) * ps <= vis_start_h[r] && to[i] == from[i]) continue;   // shared
+        if (written.has(to[i])) return LAST_ERR_INVALID;
+        written.add(to[i]);
       }
     }
+    bool both = false;
+    for (int32_t r = 0; r < R; ++r) {
+      const int32_t *from = src->table_h + (int64_t)r * src->max_pages;
+      const int32_t n = (int32_t)(((int64_t)src->lens_h[r] + ps - 1) / ps);
+      for (int32_t i = 0; i < n; ++i) both |= written.has(from[i]);
+    }
+    if (both) return LAST_ERR_INVALID;
   }
   const int64_t v = piece_elems(c->dtype);
   a.k = c->k, a.v = c->v;
@@ -850,16 +854,16 @@ last_status last_cache_copy(const last_cache *c, int32_t n, const int32_t *src, 
   if (n == 0) return LAST_OK;
   if (!src || !src_h || !dst || !dst_h) return LAST_ERR_INVALID;
   {
-    PageSet read(c->n_pages), written(c->n_pages);
-    if (!read.ok() || !written.ok()) return LAST_ERR_UNSUPPORTED;
+    PageSet written(c->n_pages);
+    if (!written.ok()) return LAST_ERR_UNSUPPORTED;
     for (int32_t i = 0; i < n; ++i) {
       if (src_h[i] < 0 || src_h[i] >= c->n_pages || dst_h[i] < 0 || dst_h[i] >= c->n_pages) return LAST_ERR_INVALID;
-      read.add(src_h[i]);
-    }
-    for (int32_t i = 0; i < n; ++i) {
-      if (read.has(dst_h[i]) || written.has(dst_h[i])) return LAST_ERR_INVALID;
+      if (written.has(dst_h[i])) return LAST_ERR_INVALID;
       written.add(dst_h[i]);
     }
+    bool both = false;
+    for (int32_t i = 0; i < n; ++i) both |= written.has(src_h[i]);
+    if (both) return LAST_ERR_INVALID;
   }
   const int64_t v = piece_elems(c->dtype);
   CopyArgs a{};
