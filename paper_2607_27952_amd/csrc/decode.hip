@@ -504,21 +504,26 @@ namespace last {
 // How a call is laid out: by the bounds of the lengths alone, so that a
 // captured call may be replayed with any lengths within them.
 //
-// Split or not, in steps: one block a unit ends after about `fair` steps (what
-// a compute unit gets if all get the same) and a tail, the longest unit's
-// excess over the mean, and not before the longest unit. Splitting takes
-// `fair` and the join, which costs about what 4 steps of an idle chip do (3
-// us); the tenth is for its blocks' search of their start. Both, split first:
-//   64 sequences of 640, 32 + 32 heads       110 us   104
-//    8 of 4096, 32 + 32 heads                 87       81
-//  200 of 8 to 700, 32 on 8 heads             45       41
-//    1 of 104, fp32, 16 + 16 heads of 64     9.8      6.7
-//    1 of 640, 28 on 4 heads                10.0     11.3
-//   16 of 1000, 28 on 4 heads               15.2     20.4
-//    8 of 16512, 28 on 4 heads                54      452
-//  128 of 288 to 16640, 12 on 2 heads         90      230
+// Split or not, in steps: one block a unit ends not before the longest unit,
+// and after about `fair` steps (what a compute unit gets if all get the same)
+// and half the longest's excess over the mean. Splitting takes `fair` and the
+// join, which costs about what 3 steps of an idle chip do; the tenth is for
+// its blocks' search of their start. More waves a block do not shorten a unit:
+// one compute unit reads some 40 GB/s, whatever it has in flight. Both, split
+// first, us:
+//   64 sequences of 640, 32 + 32 heads       110   104
+//    8 of 4096, 32 + 32 heads                 86    81
+//    4 of 1000, 32 + 32 heads               18.6  20.6
+//  200 of 8 to 700, 32 on 8 heads             43    40
+//   32 of 500, 32 on 8 heads                19.3  15.0
+//    1 of 104, fp32, 16 + 16 heads of 64     9.4   6.9
+//    4 of 300, 28 on 4 heads                 9.7   9.0
+//    1 of 640, 28 on 4 heads                 9.7  13.5
+//   16 of 1000, 28 on 4 heads               14.8  20.2
+//    8 of 16512, 28 on 4 heads                54   455
+//  128 of 288 to 16640, 12 on 2 heads         89   229
 // A split call has two blocks a compute unit, what its registers let live
-// there: with one the ragged 200 take 57 us for 45, with four the 8 of 16512
+// there: with one the ragged 200 take 57 us for 44, with four the 8 of 16512
 // take 58 for 54.
 //
 // Keys of two KV heads beside each other in memory go to one block: 8 of 16512
@@ -539,8 +544,8 @@ DecodePlan make_decode_plan(const last_cache *c, const last_pages *p, int32_t Hq
   total *= per_seq;
   const int64_t longest = (d.max_len + step - 1) / step;
   const int64_t room = 2 * device_cus();   // blocks the chip holds at once
-  const int64_t fair = total / device_cus(), tail = longest - total / units;
-  d.split = total > units && 10 * std::max(longest, fair + tail) > 11 * fair + 40;
+  const int64_t fair = 10 * total / device_cus(), tail = 10 * longest - 10 * total / units;   // in tenths
+  d.split = total > units && std::max(10 * longest, fair + tail / 2) > fair + fair / 10 + 30;
   d.blocks = std::max<int64_t>(1, d.split ? std::min(total, room) : units);
   d.steps = units * longest;
   return d;
