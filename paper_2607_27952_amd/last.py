@@ -10,6 +10,7 @@ from __future__ import annotations
 import contextlib
 import ctypes
 import os
+import struct
 from dataclasses import dataclass
 from typing import Optional
 
@@ -635,25 +636,24 @@ class Rotary:
         return Rotary(inv_freq=f, axis=_i32_dev(a, device), axis_h=a, n_axes=n, adjacent=bool(adjacent))
 
 
+_heads = struct.Struct("Pqq").pack   # a last_heads
+
+
 def _rows(t: torch.Tensor, dev: int, dtype, G: int, T: int, H, D: int, what: str):
-    """t [G][T][H][D] (H None: any) as the three numbers of a last_heads, and its heads."""
+    """t [G][T][H][D] (H None: any) as the bytes of its last_heads, and its heads."""
     if t.dtype is not dtype or t.get_device() != dev or t.dim() != 4:
         raise ValueError(f"{what} must be [G][T][heads][Dh], of the dtype and on the device of the call")
     g, n, h, d = t.shape
     ls, ts, hs, es = t.stride()
     if g != G or n != T or d != D or (h != H and H is not None) or es != 1 or (hs != D and h > 1):
         raise ValueError(f"{what} must be [{G}][{T}][{'heads' if H is None else H}][{D}] with contiguous heads")
-    return (t.data_ptr(), ls, ts), h
+    return _heads(t.data_ptr(), ls, ts), h
 
 
 def _rows_like(t: torch.Tensor, T: int, H: int, D: int):
     """A new contiguous tensor of t's shape, and its last_heads."""
     out = torch.empty_like(t, memory_format=torch.contiguous_format)
-    return out, (out.data_ptr(), T * H * D, H * D)
-
-
-_FourHeads = ctypes.c_int64 * 12   # four last_heads
-_NO_HEADS = (0, 0, 0)
+    return out, _heads(out.data_ptr(), T * H * D, H * D)
 
 
 def _positions(pos: torch.Tensor, rot: Rotary, T: int, dev: int) -> int:
@@ -676,7 +676,7 @@ def rotary(rot: Rotary, pos: torch.Tensor, q: Optional[torch.Tensor], k: Optiona
         code = _dtype_code(x)
         G, T, _, D = x.shape
         at = _positions(pos, rot, T, dev)
-        qr = qo = kr = ko = _NO_HEADS
+        qr = qo = kr = ko = None
         Hq = Hkv = 0
         if q is not None:
             qr, Hq = _rows(q, dev, dtype, G, T, None, D, "q")
@@ -690,9 +690,7 @@ def rotary(rot: Rotary, pos: torch.Tensor, q: Optional[torch.Tensor], k: Optiona
                 k_out, ko = _rows_like(k, T, Hkv, D)
             else:
                 ko, _ = _rows(k_out, dev, dtype, G, T, Hkv, D, "k_out")
-        h4 = _FourHeads(*qr, *kr, *qo, *ko)
-        p = ctypes.addressof(h4)
-        st = lib().last_rotary(rot._at[1 if inverse else 0], code, G, T, Hq, Hkv, D, at, p, p + 24, p + 48, p + 72,
+        st = lib().last_rotary(rot._at[1 if inverse else 0], code, G, T, Hq, Hkv, D, at, qr, kr, qo, ko,
                                _raw_stream(dev, stream))
     if st != LAST_OK:
         raise LastError(st, "last_rotary")
@@ -712,8 +710,8 @@ def rotary_append(rot: Optional[Rotary], cache: Cache, pages: Pages, pos: Option
         G, T = k.shape[:2]
         kr, _ = _rows(k, dev, dtype, G, T, cache._Hkv, D, "k")
         vr, _ = _rows(v, dev, dtype, G, T, cache._Hkv, D, "v")
-        qr = qo = _NO_HEADS
-        Hq = at = 0
+        qr = qo = at = None
+        Hq = 0
         if q is not None:
             qr, Hq = _rows(q, dev, dtype, G, T, None, D, "q")
             if q_out is None:
@@ -732,11 +730,9 @@ def rotary_append(rot: Optional[Rotary], cache: Cache, pages: Pages, pos: Option
             _dev_i32(cu_new, dev, "cu_new", (pages.R + 1,))
         elif cu_new is not None:
             raise ValueError("cu_new needs cu_new_h")
-        h4 = _FourHeads(*qr, *qo, *kr, *vr)
-        p = ctypes.addressof(h4)
         st = lib().last_rotary_append(rot._at[0] if rot is not None else None, cache._at, layer, G, pages._at, T,
                                       None if cu is None else cu_new.data_ptr(), None if cu is None else cu.tobytes(),
-                                      Hq, at, p, p + 24, p + 48, p + 72, _raw_stream(dev, stream))
+                                      Hq, at, qr, qo, kr, vr, _raw_stream(dev, stream))
     if st != LAST_OK:
         raise LastError(st, "last_rotary_append")
     return q_out
