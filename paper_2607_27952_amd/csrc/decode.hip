@@ -522,6 +522,11 @@ namespace last {
 //   16 of 1000, 28 on 4 heads               14.8  20.2
 //    8 of 16512, 28 on 4 heads                54   455
 //  128 of 288 to 16640, 12 on 2 heads         89   229
+// The bounds may be far above the lengths, which an unsplit call would meet
+// with one long block: it is not used past 16 steps. 64 sequences with bounds
+// of 8192, 28 on 4 heads, one of them that long and 500 tokens in the others:
+// split 23 us, not split 116 (what this costs is the 5 of the second line).
+//
 // A split call has two blocks a compute unit, what its registers let live
 // there: with one the ragged 200 take 57 us for 44, with four the 8 of 16512
 // take 58 for 54.
@@ -545,7 +550,7 @@ DecodePlan make_decode_plan(const last_cache *c, const last_pages *p, int32_t Hq
   const int64_t longest = (d.max_len + step - 1) / step;
   const int64_t room = 2 * device_cus();   // blocks the chip holds at once
   const int64_t fair = 10 * total / device_cus(), tail = 10 * longest - 10 * total / units;   // in tenths
-  d.split = total > units && std::max(10 * longest, fair + tail / 2) > fair + fair / 10 + 30;
+  d.split = total > units && (longest > 16 || std::max(10 * longest, fair + tail / 2) > fair + fair / 10 + 30);
   d.blocks = std::max<int64_t>(1, d.split ? std::min(total, room) : units);
   d.steps = units * longest;
   return d;

@@ -233,3 +233,19 @@ def test_captured_prune_and_copy():
             e = ref.prune(p, src, dst, ps, old)
             e[:, pages], e[:, pages + 1] = e[:, src[0, 0]], e[:, dst[1, 0]]
             assert same_bits(x.cpu(), e)
+
+
+@pytest.mark.parametrize("bound", [2048, 8192])
+def test_decode_one_long_among_short(bound):
+    """Bounds that say nothing of the lengths: one sequence as long as they allow, the others short."""
+    R, ps, Hkv, Dh = 64, 64, 4, 128
+    gg, rng = gen(9), np.random.default_rng(9)
+    lens = rng.integers(0, 300, R)
+    lens[41] = bound
+    pages = 200
+    table = rng.integers(0, pages, (R, bound // ps)).astype(np.int32)      # pages may be shared: they are only read
+    kp, vp = (ref.pool(gg, 1, pages, Hkv, ps, Dh, BF) for _ in "kv")
+    q = torch.randn((R, 28, Dh), generator=gg).to(BF)
+    seqs = last.Pages(lens_h=np.full(R, bound), table=torch.from_numpy(table).cuda(),
+                      lens=torch.from_numpy(lens.astype(np.int32)).cuda())
+    check(last.Cache(kp.cuda(), vp.cuda()), seqs, q, ref.decode(q, kp[0], vp[0], table, lens), lens, 0)
