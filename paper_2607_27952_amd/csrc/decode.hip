@@ -188,8 +188,8 @@ struct Share {
   }
 };
 // Inclusive sums over a wave, whose sum is returned in `sum`: DPP shifts inside
-// rows of 16 lanes (a tenth of the time of shuffles, which pass through LDS and
-// would stand before a block's first load), then the rows' ends.
+// rows of 16 lanes, then the rows' ends. It stands before a block's first load:
+// one sequence of 2048 tokens 9.6 us, 10.0 with shuffles, which pass LDS.
 __device__ __forceinline__ int wave_scan(int v, int *sum) {
   v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, true);
   v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, true);
