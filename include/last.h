@@ -512,10 +512,10 @@ size_t last_decode_attention_workspace(const last_cache *c, const last_pages *p,
  *   ws         last_decode_attention_workspace bytes, 256-byte aligned; calls
  *              that may overlap in time need their own
  * Logits, softmax statistics, probabilities and sums are held in fp32 (for
- * bf16 caches a probability enters the value product as the sum of two bf16
- * numbers, within 2^-16 of it; an infinite value may so give NaN instead of
- * infinity). A long cache is split over blocks whose
- * partial results are joined in a fixed order.
+ * bf16 caches a probability enters the value product as the sum of three bf16
+ * numbers, exactly; as some of them may be 0, an infinite value may give NaN
+ * instead of infinity). A long cache is split over blocks whose partial
+ * results are joined in a fixed order.
  */
 last_status last_decode_attention(const last_cache *c, int32_t layer, const last_pages *p,
                                   int32_t Hq, float scale, const void *q, int64_t q_stride,
