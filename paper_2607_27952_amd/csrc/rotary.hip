@@ -144,41 +144,47 @@ __global__ __launch_bounds__(256) void k_rotary(RotaryArgs a) {
     const bool halves = !a.adjacent && ic < half;
     const int p0 = halves ? ic : 2 * ic;
     const int p1 = halves ? ic + half : p0 + 1;
-    float x[VEC], y[VEC];
     typedef typename Piece<T>::vec vec;
-    const vec *s0 = reinterpret_cast<const vec *>(src + p0 * VEC), *s1 = reinterpret_cast<const vec *>(src + p1 * VEC);
-    Piece<T>::get(*s0, x);
-    Piece<T>::get(*s1, y);
-    if (turn && halves) {
+    vec u0 = *reinterpret_cast<const vec *>(src + p0 * VEC), u1 = *reinterpret_cast<const vec *>(src + p1 * VEC);
+    // What is not turned is stored as it was read: through fp32 and back a bf16
+    // signalling NaN would change.
+    if (turn && (halves || (a.adjacent && p0 * VEC < 2 * a.F))) {
+      float x[VEC], y[VEC];
+      Piece<T>::get(u0, x);
+      Piece<T>::get(u1, y);
+      if (halves) {
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) {
-        const float c = cs[t][p0 * VEC + e], s = sn[t][p0 * VEC + e];
-        const float u = x[e] * c - y[e] * s;
-        y[e] = y[e] * c + x[e] * s;
-        x[e] = u;
-      }
-    } else if (turn && a.adjacent && p0 * VEC < 2 * a.F) {
+        for (int e = 0; e < VEC; ++e) {
+          const float c = cs[t][p0 * VEC + e], s = sn[t][p0 * VEC + e];
+          const float u = x[e] * c - y[e] * s;
+          y[e] = y[e] * c + x[e] * s;
+          x[e] = u;
+        }
+      } else {
 #pragma unroll
-      for (int e = 0; e < VEC; e += 2) {
-        const int f = (p0 * VEC + e) / 2, f1 = f + VEC / 2;
-        const float u = x[e] * cs[t][f] - x[e + 1] * sn[t][f];
-        x[e + 1] = x[e + 1] * cs[t][f] + x[e] * sn[t][f];
-        x[e] = u;
-        const float w = y[e] * cs[t][f1] - y[e + 1] * sn[t][f1];
-        y[e + 1] = y[e + 1] * cs[t][f1] + y[e] * sn[t][f1];
-        y[e] = w;
+        for (int e = 0; e < VEC; e += 2) {
+          const int f = (p0 * VEC + e) / 2, f1 = f + VEC / 2;
+          const float u = x[e] * cs[t][f] - x[e + 1] * sn[t][f];
+          x[e + 1] = x[e + 1] * cs[t][f] + x[e] * sn[t][f];
+          x[e] = u;
+          const float w = y[e] * cs[t][f1] - y[e + 1] * sn[t][f1];
+          y[e + 1] = y[e + 1] * cs[t][f1] + y[e] * sn[t][f1];
+          y[e] = w;
+        }
       }
+      u0 = Piece<T>::put(x);
+      u1 = Piece<T>::put(y);
     }
     // Past the caches where the rows go to pages (appending 108000 tokens of
     // 12 + 2 heads 154 against 160 us), not where they stay rows (132096 tokens
     // of 28 + 4 heads 354 against 363).
     vec *d0 = reinterpret_cast<vec *>(dst + p0 * VEC), *d1 = reinterpret_cast<vec *>(dst + p1 * VEC);
     if (APPEND) {
-      __builtin_nontemporal_store(Piece<T>::put(x), d0);
-      __builtin_nontemporal_store(Piece<T>::put(y), d1);
+      __builtin_nontemporal_store(u0, d0);
+      __builtin_nontemporal_store(u1, d1);
     } else {
-      *d0 = Piece<T>::put(x);
-      *d1 = Piece<T>::put(y);
+      *d0 = u0;
+      *d1 = u1;
     }
   }
 }
