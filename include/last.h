@@ -488,8 +488,11 @@ last_status last_rotary_append(const last_rotation *rot, const last_cache *c, in
                                const last_heads *q, const last_heads *q_out, const last_heads *k,
                                const last_heads *v, void *stream);
 
-/* Workspace bytes last_decode_attention needs: a function of lens_h, which
- * need not be exact (0 if the arguments are invalid, at least 256 otherwise). */
+/* Workspace bytes last_decode_attention needs (0 if the arguments are invalid,
+ * at least 256 otherwise): a function of the cache's shape, Hq, the number of
+ * sequences and lens_h, which need not be exact. It does not fall as sequences
+ * or longer bounds are added, so a workspace for the most sequences and the
+ * longest bounds serves every call below them. */
 size_t last_decode_attention_workspace(const last_cache *c, const last_pages *p, int32_t Hq);
 
 /*

@@ -746,12 +746,15 @@ static last_status check_decode(const last_cache *c, const last_pages *p, int32_
   return LAST_OK;
 }
 
+// The workspace of a split call. Its size never falls as bounds or sequences
+// are added, which the choice between split and not split does not do: a query
+// answers with it for either.
 static size_t decode_ws(const last_cache *c, const last_pages *p, const DecodePlan &d, void *ws, DecodeArgs *a) {
   Carver cv(ws);
-  const size_t rows = d.split ? (size_t)d.blocks * 2 * d.heads_of_block * 16 : 0;   // two parts of a block
+  const size_t rows = (size_t)d.shares * 2 * d.heads_of_block * 16;   // two parts of a block
   a->part_o = cv.take<float>(rows * c->Dh);
   a->part_ml = cv.take<float2>(rows);
-  a->info = cv.take<int2>(d.split ? (size_t)p->R * (c->Hkv / d.heads_of_block) * d.head_tiles : 0);
+  a->info = cv.take<int2>((size_t)p->R * (c->Hkv / d.heads_of_block) * d.head_tiles);
   return std::max<size_t>(256, cv.size());
 }
 
@@ -773,9 +776,9 @@ last_status last_decode_attention(const last_cache *c, int32_t layer, const last
   if (p->R > 1 && (q_stride < 0 || q_stride > kMaxStride / p->R || q_stride % piece_elems(c->dtype)))
     return LAST_ERR_INVALID;
   DecodeArgs a{};
-  const size_t need = decode_ws(c, p, d, nullptr, &a);
+  const size_t need = d.split ? decode_ws(c, p, d, nullptr, &a) : 256;
   if (!ws || ws_bytes < need || !aligned(ws, 256)) return LAST_ERR_WORKSPACE;
-  decode_ws(c, p, d, ws, &a);
+  if (d.split) decode_ws(c, p, d, ws, &a);
   const size_t e = c->dtype == LAST_BF16 ? 2 : 4, at = (size_t)(c->G > 1 ? layer * c->layer_stride : 0) * e;
   a.k = static_cast<const char *>(c->k) + at;
   a.v = static_cast<const char *>(c->v) + at;

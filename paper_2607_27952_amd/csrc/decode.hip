@@ -568,7 +568,8 @@ DecodePlan make_decode_plan(const last_cache *c, const last_pages *p, int32_t Hq
   const int64_t room = 2 * device_cus();   // blocks the chip holds at once
   const int64_t fair = 10 * total / device_cus(), tail = 10 * longest - 10 * total / units;   // in tenths
   d.split = total > units && (longest > 16 || std::max(10 * longest, fair + tail / 2) > fair + fair / 10 + 30);
-  d.blocks = std::max<int64_t>(1, d.split ? std::min(total, room) : units);
+  d.shares = std::max<int64_t>(1, std::min(total, room));
+  d.blocks = d.split ? d.shares : units;
   d.steps = units * longest;
   return d;
 }

@@ -304,6 +304,7 @@ struct DecodePlan {
   int32_t head_tiles, max_len, heads_of_block;
   bool split;              // the line of steps in equal shares, or a block per unit
   int64_t blocks, steps;   // steps of the line if all sequences had the longest bound
+  int64_t shares;          // blocks of the call if it is split
 };
 struct DecodeArgs {
   const void *k, *v, *q;

@@ -1,0 +1,61 @@
+"""How decode attention lays a call out by the bounds of its lengths: the workspace it asks for, and when it splits."""
+import numpy as np
+import pytest
+import torch
+
+import cache_ref as ref
+from paper_2607_27952_amd import last
+
+
+class Asked:
+    """The workspace query with made-up addresses: it follows none of them on the device."""
+
+    def __init__(self, dtype, Hkv, Hq, Dh, major, max_pages=8192):
+        ps, self.Hq, self.max_pages = 16, Hq, max_pages
+        hs, ts = (Dh, Hkv * Dh) if major else (ps * Dh, Dh)
+        page = Hkv * ps * Dh
+        self.cache = last._Cache(1, 64, ps, Hkv, Dh, dtype, 64 * page, page, hs, ts, 1 << 20, 1 << 21)
+
+    def bytes(self, lens):
+        lens = np.ascontiguousarray(lens, dtype=np.int32)
+        pages = last._Pages(len(lens), self.max_pages, 256, None, 256, lens.ctypes.data)
+        return last.lib().last_decode_attention_workspace(self.cache, pages, self.Hq)
+
+
+SHAPES = [(last.LAST_BF16, 32, 32, 128, False), (last.LAST_BF16, 4, 28, 128, True), (last.LAST_BF16, 8, 32, 64, False),
+          (last.LAST_F32, 16, 16, 64, True), (last.LAST_BF16, 1, 40, 128, False)]
+
+
+@pytest.mark.parametrize("shape", SHAPES)
+def test_workspace_covers_shorter_bounds(shape):
+    """A workspace for some bounds serves every call whose bounds are no longer, and of no more sequences."""
+    ask, rng = Asked(*shape), np.random.default_rng(3)
+    assert ask.bytes([0]) >= 256
+    for R, longest in ((64, 2048), (64, 640), (32, 1000), (1, 104), (200, 16), (8, 100000), (256, 3)):
+        for _ in range(30):
+            lens = np.full(R, longest) if rng.random() < 0.5 else rng.integers(0, longest + 1, R)
+            need = ask.bytes(lens)
+            shorter = [np.minimum(lens, rng.integers(0, longest + 1, R)), np.minimum(lens, rng.integers(0, longest + 1)), lens // 64,
+                       np.where(np.arange(R) < max(1, R // 16), lens, 10), np.where(rng.random(R) < 0.1, lens, 0)]
+            for less in shorter:
+                less = np.minimum(less, lens)
+                assert ask.bytes(less) <= need, (R, longest)
+                assert ask.bytes(less[:rng.integers(1, R + 1)]) <= need, (R, longest)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("longest,short", [(640, 10), (2048, 100)])
+def test_workspace_of_the_longest_bounds_serves_shorter_ones(longest, short):
+    """One workspace, sized once for even long bounds, in calls of ragged shorter ones."""
+    R, Hkv, Hq, Dh, ps = 64, 4, 28, 128, 16
+    gg, rng = torch.Generator().manual_seed(2), np.random.default_rng(2)
+    kp, vp = (ref.pool(gg, 1, 256, Hkv, ps, Dh, torch.bfloat16) for _ in "kv")
+    cache = last.Cache(kp.cuda(), vp.cuda())
+    table = rng.integers(0, 256, (R, longest // ps)).astype(np.int32)       # pages are only read: they may be shared
+    need = last.decode_attention_workspace(cache, last.Pages.make(table, [longest] * R), Hq)
+    ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+    q = torch.randn((R, Hq, Dh), generator=gg).bfloat16()
+    for lens in ([longest] * 4 + [short] * 60, [longest] + [0] * 63, [short] * 64, [longest] * 64):
+        got = last.decode_attention(cache, last.Pages.make(table, lens), q.cuda(), ws=ws).cpu().double()
+        out, _, bound, _ = ref.decode(q, kp[0], vp[0], table, lens)
+        assert bool(((got - out).abs() <= bound).all())
