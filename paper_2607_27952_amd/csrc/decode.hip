@@ -542,7 +542,8 @@ namespace last {
 // The bounds may be far above the lengths, which an unsplit call would meet
 // with one long block: it is not used past 16 steps. 64 sequences with bounds
 // of 8192, 28 on 4 heads, one of them that long and 500 tokens in the others:
-// split 23 us, not split 116 (what this costs is the 5 of the second line).
+// split 23 us, not split 116 (what this costs is the 5 of the second line);
+// 256 slots with bounds of 0 but for one of 20000, 12 on 2 heads: 16 and 261.
 //
 // A split call has two blocks a compute unit, what its registers let live
 // there: with one the ragged 200 take 57 us for 44, with four the 8 of 16512
@@ -567,7 +568,7 @@ DecodePlan make_decode_plan(const last_cache *c, const last_pages *p, int32_t Hq
   const int64_t longest = (d.max_len + step - 1) / step;
   const int64_t room = 2 * device_cus();   // blocks the chip holds at once
   const int64_t fair = 10 * total / device_cus(), tail = 10 * longest - 10 * total / units;   // in tenths
-  d.split = total > units && (longest > 16 || std::max(10 * longest, fair + tail / 2) > fair + fair / 10 + 30);
+  d.split = longest > 16 || (total > units && std::max(10 * longest, fair + tail / 2) > fair + fair / 10 + 30);
   d.shares = std::max<int64_t>(1, std::min(total, room));
   d.blocks = d.split ? d.shares : units;
   d.steps = units * longest;

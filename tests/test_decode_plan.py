@@ -59,3 +59,37 @@ def test_workspace_of_the_longest_bounds_serves_shorter_ones(longest, short):
         got = last.decode_attention(cache, last.Pages.make(table, lens), q.cuda(), ws=ws).cpu().double()
         out, _, bound, _ = ref.decode(q, kp[0], vp[0], table, lens)
         assert bool(((got - out).abs() <= bound).all())
+
+
+def kernels_of(call):
+    last.profile_enable(True)
+    try:
+        torch.cuda.synchronize()
+        last.profile_collect()
+        last.profile_reset()
+        got = call()
+        torch.cuda.synchronize()
+        return got, {name: n for name, (n, _) in last.profile_collect().items() if n}
+    finally:
+        last.profile_enable(False)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("R,longest,at", [(256, 6000, 77), (200, 20000, 0), (64, 2100, 63)])
+def test_a_long_sequence_among_empty_slots_is_split(R, longest, at):
+    """A padded batch whose empty slots have bounds of 0: its one long sequence is shared out among the blocks."""
+    Hkv, Hq, Dh, ps = 2, 8, 128, 16
+    gg, rng = torch.Generator().manual_seed(4), np.random.default_rng(4)
+    lens = np.zeros(R, np.int32)
+    lens[at] = longest
+    kp, vp = (ref.pool(gg, 1, 128, Hkv, ps, Dh, torch.bfloat16) for _ in "kv")
+    table = rng.integers(0, 128, (R, -(-longest // ps))).astype(np.int32)
+    q = torch.randn((R, Hq, Dh), generator=gg).bfloat16()
+    cache, pages = last.Cache(kp.cuda(), vp.cuda()), last.Pages.make(table, lens)
+    got, kernels = kernels_of(lambda: last.decode_attention(cache, pages, q.cuda(), want_lse=True))
+    assert kernels == {"decode": 1, "decode_join": 1}
+    out, lse, bound, lbound = ref.decode(q, kp[0], vp[0], table, lens)
+    assert bool(((got[0].cpu().double() - out).abs() <= bound).all())
+    assert float((got[1][at].cpu().double() - lse[at]).abs().max()) <= float(lbound[at].max())
+    rest = np.arange(R) != at
+    assert bool((got[0][rest] == 0).all()) and bool((got[1][rest] == -float("inf")).all())
