@@ -216,7 +216,7 @@ static void shape(RotaryArgs *a, int items, bool append, int cus, int64_t *block
   const int heads = a->Hq + (append ? 2 : 1) * a->Hkv;
   const int want = std::max(1, std::min(kTokens, (2 * (append ? 512 : 256) + heads * items) / (2 * heads * items)));
   a->tokens = (int64_t)a->T * a->G >= (int64_t)want * 4 * cus ? want : 1;
-  const int64_t b = (int64_t)((a->T + a->tokens - 1) / a->tokens) * a->G;
+  const int64_t b = ((int64_t)a->T + a->tokens - 1) / a->tokens * a->G;
   int64_t parts = std::max<int64_t>(1, (2 * cus) / b);
   a->parts = (int32_t)std::min<int64_t>(parts, std::max(1, heads / 8));
   *blocks = b * a->parts;
