@@ -538,6 +538,8 @@ last_status last_decode_attention(const last_cache *c, int32_t layer, const last
  *   kept, cu_keep      as from diverse_select (0 <= K_r <= N_r): an index
  *              outside [0, N_r) yields a zero-filled row
  *   new_lens   optional [R] device out: the new lengths; not src->lens
+ * R below 2^23 and R times the longest new length below 2^28 are always
+ * taken; past that LAST_ERR_UNSUPPORTED may be returned.
  * Pages that dst writes must be listed once and not by src (LAST_ERR_INVALID):
  * the source stays whole, so other sequences may share its pages. The
  * exception is a page wholly before vis_start that both tables name at the

@@ -555,7 +555,6 @@ last_status last_connector(last_dtype dtype, int64_t K, int32_t Dv, int32_t Dh, 
 namespace last {
 
 constexpr int64_t kMaxStride = (int64_t)1 << 48;
-constexpr int64_t kMaxBlocks = (int64_t)1 << 24;   // 256 threads each: a launch holds under 2^32
 
 static int64_t piece_elems(last_dtype dt) { return dt == LAST_BF16 ? 8 : 4; }
 static int32_t log2_of(int32_t x) { return 31 - __builtin_clz((unsigned)x); }

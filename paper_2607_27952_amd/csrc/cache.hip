@@ -64,7 +64,7 @@ __global__ __launch_bounds__(256) void k_cache_prune(PruneArgs a) {
   int64_t b = blockIdx.x;
   const int tile = (int)(b % a.tiles);
   b /= a.tiles;
-  const int pools = 2 * a.G, sets = (pools + a.span - 1) / a.span;
+  const int pools = 2 * a.G, sets = (pools - 1) / a.span + 1;
   const int first = (int)(b % sets) * a.span, last = min(pools, first + a.span);   // pools: keys and values of a layer
   const int r = (int)(b / sets);
   const int len = a.lens[r], vis = a.vis_start[r];
@@ -141,13 +141,26 @@ hipError_t launch_cache_copy(const CopyArgs &a, int64_t blocks, hipStream_t s) {
 // goes to) then serves all of them. Eight sequences of 16384 visual tokens to
 // 1024, 4 layers of 4 heads: 32 us, one pool a block 40; 32 sequences of 288 to
 // 16384 to a ninth, 4 layers of 2 heads: 26, one pool a block 53.
+// Tiles are counted by the longest sequence, whose blocks the shorter ones
+// leave at once. Where a launch does not hold so many, a block takes every pool
+// (as many as 32 bits count the pieces of), then the most tokens.
 int64_t prune_blocks(PruneArgs *a) {
-  a->rows = std::max(2, std::min(kRowsPrune, 256 / std::min(256, a->Hkv << a->lc)));
-  a->tiles = std::max(1, (a->max_new + a->rows - 1) / a->rows);
-  const int pools = 2 * a->G;
-  const int64_t all = (int64_t)a->R * pools * a->tiles;
-  a->span = (int32_t)std::max<int64_t>(1, std::min<int64_t>({pools, 256 * kItems / ((a->Hkv * a->rows) << a->lc), all / (4 * device_cus())}));
-  return (int64_t)a->R * a->tiles * ((pools + a->span - 1) / a->span);
+  const int64_t pools = 2 * (int64_t)a->G;
+  auto set_rows = [a](int rows) {
+    a->rows = rows;
+    a->tiles = std::max(1, (a->max_new + rows - 1) / rows);
+  };
+  auto pieces = [a] { return ((int64_t)a->Hkv * a->rows) << a->lc; };
+  auto set_span = [a, pools](int64_t span) { a->span = (int32_t)std::max<int64_t>(1, std::min(pools, span)); };
+  auto blocks = [a, pools] { return (int64_t)a->R * a->tiles * ((pools + a->span - 1) / a->span); };
+  set_rows(std::max(2, std::min(kRowsPrune, 256 / std::min(256, a->Hkv << a->lc))));
+  set_span(std::min(256 * kItems / pieces(), (int64_t)a->R * pools * a->tiles / (4 * device_cus())));
+  if (blocks() >= kMaxBlocks) set_span(((int64_t)1 << 31) / pieces());
+  if (blocks() >= kMaxBlocks) {
+    set_rows(kRowsPrune);
+    set_span(((int64_t)1 << 31) / pieces());
+  }
+  return blocks();
 }
 
 hipError_t launch_cache_prune(const PruneArgs &a, int64_t blocks, hipStream_t s) {

@@ -280,6 +280,8 @@ hipError_t launch_connector(int64_t K, int32_t Dv, int32_t Dh, int32_t Do, float
                             const void *w2, const float *b2, void *out, void *xn, void *hid,
                             hipStream_t s);
 
+constexpr int64_t kMaxBlocks = (int64_t)1 << 24;   // of 256 threads: a launch holds under 2^32 of them
+
 // ------------------------------------------------------------ rotary (rotary.hip)
 struct RotaryArgs {
   const float *inv_freq;

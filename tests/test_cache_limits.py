@@ -1,5 +1,6 @@
 """Calls at the limits of what one launch holds, without a GPU where they are refused on the host: nothing they
 were given is followed or written."""
+import numpy as np
 import pytest
 
 from paper_2607_27952_amd import last
@@ -29,3 +30,22 @@ def test_append_refuses_the_most_tokens(T):
     for n in ("k", "v"):
         c.heads[n] = last._Heads(c.mem["q"].p, 0, 0)
     assert c.append() == UNS and c.untouched()
+
+
+def test_prune_refuses_more_tiles_than_a_launch_holds():
+    """2^14 sequences whose longest new length is 2^15: 2^24 blocks of 32 tokens, whatever the others keep."""
+    R, n = 1 << 14, 1 << 15
+    c = Call()
+    c.cache.page_size, c.cache.head_stride, c.cache.page_stride = 1024, 1024 * 64, 4 * 1024 * 64
+    c.cache.n_pages = 32 + R + 32
+    c.cache.layer_stride = c.cache.n_pages * c.cache.page_stride
+    c.lens, c.later = np.full(R, 40, np.int32), np.full(R, 40, np.int32)
+    c.lens[3] = c.later[3] = n
+    c.table = np.tile(np.arange(32, dtype=np.int32), (R, 1))
+    c.into = np.zeros((R, 32), np.int32)
+    c.into[:, 0] = 64 + np.arange(R)
+    c.into[3] = 32 + np.arange(32)
+    for p, table, lens in ((c.pages, c.table, c.lens), (c.dst, c.into, c.later)):
+        p.R, p.max_pages, p.table_h, p.lens_h = R, 32, table.ctypes.data, lens.ctypes.data
+    c.vis, c.cu_vis, c.cu_keep = np.zeros(R, np.int32), np.zeros(R + 1, np.int32), np.zeros(R + 1, np.int32)
+    assert c.prune() == UNS and c.untouched()
