@@ -379,8 +379,8 @@ last_status last_connector(last_dtype dtype, int64_t K, int32_t Dv, int32_t Dh, 
  *   strides in elements; v has the same layout.
  * Any order of layer, page, head and token is accepted as long as no two rows
  * of Dh elements overlap (the strides nest) and every row is 16-byte aligned.
- * page_size is a power of two in [8, 1024] and Dh 64 or 128 (others:
- * LAST_ERR_UNSUPPORTED). k and v must not overlap each other.
+ * page_size is a power of two in [8, 1024], Dh 64 or 128 and Hkv at most 65536
+ * (others: LAST_ERR_UNSUPPORTED). k and v must not overlap each other.
  */
 typedef struct last_cache {
   int32_t G, n_pages, page_size, Hkv, Dh;
@@ -445,9 +445,12 @@ typedef struct last_heads {
 /*
  * The rotary embedding that last_prefill_attention and the score calls expect
  * their q and k to carry: q_out = rot(q), k_out = rot(k).
- *   G, T       layers and tokens (T >= 0); every layer has the same positions
- *   Hq, Hkv    heads of q and k; one of them may be 0, its rows are then not
- *              read and may be NULL
+ *   G, T       layers and tokens (T >= 0); every layer has the same positions.
+ *              G T below 2^24 is always taken; past that
+ *              LAST_ERR_UNSUPPORTED may be returned
+ *   Hq, Hkv    heads of q and k, at most 65536 each (LAST_ERR_UNSUPPORTED
+ *              otherwise); one of them may be 0, its rows are then not read
+ *              and may be NULL
  *   Dh         64 or 128 (others: LAST_ERR_UNSUPPORTED)
  *   dtype      of all rows (LAST_F32 or LAST_BF16); turned in fp32, rounded
  *              once, to nearest even
@@ -471,7 +474,8 @@ last_status last_rotary(const last_rotation *rot, last_dtype dtype, int32_t G, i
  *   c          the cache; layers [layer, layer + G) are written, row g of k
  *              and v into layer + g
  *   p          sequences; lens_h bounds lens from above, table_h may be NULL
- *   T          new tokens of all sequences
+ *   G, T       layers and new tokens of all sequences, limited as in
+ *              last_rotary
  *   cu_new     [R+1] CSR offsets of each sequence's new tokens, which end at
  *              T (device and host copy); both NULL: one token per sequence, T = R
  *   pos        [n_axes][T] positions of the rotation (not of the cache)
@@ -506,7 +510,9 @@ size_t last_decode_attention_workspace(const last_cache *c, const last_pages *p,
  *   layer      the layer read
  *   p          lens_h bounds lens from above (it shapes the launch; a captured
  *              call may be replayed with any lens within it); table_h may be NULL
- *   Hq         query heads, a multiple of the cache's Hkv
+ *   Hq         query heads, a multiple of the cache's Hkv. R Hq below 2^22 with
+ *              R Hq times the longest bound below 2^35 is always taken; past
+ *              that LAST_ERR_UNSUPPORTED may be returned
  *   scale      sigma; <= 0 selects 1/sqrt(Dh)
  *   q          [R][Hq][Dh] after the rotary embedding, row r at r * q_stride
  *              elements, 16-byte aligned
@@ -556,6 +562,8 @@ last_status last_cache_prune(const last_cache *c, const last_pages *src, const l
  * to page dst[i] (a forked sequence's last, partly filled page; pages moved
  * together). No page may be a target twice, or both source and target
  * (LAST_ERR_INVALID). src and dst: [n] device arrays with host copies, n >= 0.
+ * Hkv page_size is at most 2^24 and 2 G n ceil(Hkv page_size Dh elt / 4096), elt
+ * an element's bytes, below 2^24 (some 64 GiB; LAST_ERR_UNSUPPORTED otherwise).
  */
 last_status last_cache_copy(const last_cache *c, int32_t n, const int32_t *src, const int32_t *src_h,
                             const int32_t *dst, const int32_t *dst_h, void *stream);

@@ -49,3 +49,45 @@ def test_prune_refuses_more_tiles_than_a_launch_holds():
         p.R, p.max_pages, p.table_h, p.lens_h = R, 32, table.ctypes.data, lens.ctypes.data
     c.vis, c.cu_vis, c.cu_keep = np.zeros(R, np.int32), np.zeros(R + 1, np.int32), np.zeros(R + 1, np.int32)
     assert c.prune() == UNS and c.untouched()
+
+
+def test_copy_refuses_more_pieces_than_a_launch_holds():
+    """Pages of 512 KB a layer: 2 layers of 32768 pages are 64 GiB."""
+    c = Call()
+    c.cache.page_size, c.cache.head_stride, c.cache.page_stride = 1024, 1024 * 64, 4 * 1024 * 64
+    n = 1 << 15
+    c.cache.n_pages = 2 * n
+    c.cache.layer_stride = c.cache.n_pages * c.cache.page_stride
+    ids = np.arange(2 * n, dtype=np.int32)
+    c.src_h, c.dst_h, c.a["n"] = ids[:n].copy(), ids[n:].copy(), n
+    assert c.copy() == UNS and c.untouched()
+    c.cache.page_size, c.cache.Hkv, c.a["n"] = 512, 1 << 16, 1            # and a page of 2^25 rows
+    c.cache.head_stride, c.cache.page_stride = 512 * 64, 512 * 64 << 16
+    c.cache.layer_stride = c.cache.n_pages * c.cache.page_stride
+    assert c.copy() == UNS and c.untouched()
+
+
+def decode_limits(R, Hkv, Hq, bound):
+    c = Call()
+    c.cache.Hkv, c.cache.page_size, c.cache.head_stride, c.cache.page_stride = Hkv, 1024, 1024 * 64, Hkv * 1024 * 64
+    c.cache.layer_stride = c.cache.n_pages * c.cache.page_stride
+    c.lens = np.full(R, bound, np.int32)
+    c.pages.R, c.pages.max_pages, c.pages.table_h, c.pages.lens_h = R, max(1, bound // 1024), None, c.lens.ctypes.data
+    c.a["Hq"], c.a["q_stride"] = Hq, Hq * 64
+    return c
+
+
+@pytest.mark.parametrize("R,Hkv,Hq,bound", [(1 << 18, 64, 64, 1), (1 << 17, 64, 64, 1 << 19), (1 << 8, 1 << 14, 1 << 14, 1)])
+def test_decode_refuses_more_than_a_launch_holds(R, Hkv, Hq, bound):
+    """2^24 query heads, 2^23 of them with 4096 steps and more each, 2^22 units."""
+    c = decode_limits(R, Hkv, Hq, bound)
+    assert c.decode() == UNS and c.untouched()
+    assert last.lib().last_decode_attention_workspace(c.cache, c.pages, Hq) == 0
+
+
+def test_decode_takes_what_is_always_taken():
+    """Just under the bounds that are always taken: the query answers."""
+    for R, Hkv, Hq, bound in (((1 << 16) - 1, 1, 64, 1 << 13), (1 << 10, 4, 4, 1 << 22), ((1 << 22) - 1, 1, 1, 1 << 13)):
+        c = decode_limits(R, Hkv, Hq, bound)
+        assert R * Hq < 2 ** 22 and R * Hq * bound < 2 ** 35
+        assert last.lib().last_decode_attention_workspace(c.cache, c.pages, Hq) >= 256
