@@ -396,13 +396,15 @@ typedef struct last_cache {
  *              (LAST_ERR_UNSUPPORTED otherwise)
  *   table      [R][max_pages] device: token t of sequence r lies in page
  *              table[r][t / page_size], the same page in every layer. Entries
- *              behind a sequence's last page are never read.
+ *              behind the last page of lens[r] tokens are never read.
  *   table_h    host copy, or NULL where the call allows it
  *   lens       [R] device: tokens of each sequence, 0 allowed
  *   lens_h     [R] host: what lens holds, or (calls that say so) a bound of it
  * The page table and the lengths may change between the replays of a captured
- * call, so the kernels check them too: a page outside [0, n_pages) or a
- * length outside its bound is never followed.
+ * call, so the kernels check them too: a page outside [0, n_pages) is never
+ * followed, and lengths are cut to [0, max(lens_h)]. That is the longest bound
+ * of the call: a length above its own sequence's bound but not above that is
+ * taken as it stands, through entries of table that the host did not check.
  */
 typedef struct last_pages {
   int32_t R, max_pages;
@@ -509,7 +511,8 @@ size_t last_decode_attention_workspace(const last_cache *c, const last_pages *p,
  * the cache (within its length) gives NaN in both.
  *   layer      the layer read
  *   p          lens_h bounds lens from above (it shapes the launch; a captured
- *              call may be replayed with any lens within it); table_h may be NULL
+ *              call may be replayed with any lens up to its maximum); table_h
+ *              may be NULL
  *   Hq         query heads, a multiple of the cache's Hkv. R Hq below 2^22 with
  *              R Hq times the longest bound below 2^35 is always taken; past
  *              that LAST_ERR_UNSUPPORTED may be returned

@@ -93,3 +93,24 @@ def test_a_long_sequence_among_empty_slots_is_split(R, longest, at):
     assert float((got[1][at].cpu().double() - lse[at]).abs().max()) <= float(lbound[at].max())
     rest = np.arange(R) != at
     assert bool((got[0][rest] == 0).all()) and bool((got[1][rest] == -float("inf")).all())
+
+
+@pytest.mark.gpu
+def test_lengths_are_cut_to_the_longest_bound():
+    """A length above its own sequence's bound is taken up to the longest bound of the call, by decode and append."""
+    Hkv, Dh, ps = 2, 64, 16
+    gg = torch.Generator().manual_seed(6)
+    kp, vp = (ref.pool(gg, 1, 24, Hkv, ps, Dh, torch.bfloat16) for _ in "kv")
+    table = np.arange(21, dtype=np.int32).reshape(3, 7)
+    q = torch.randn((3, 4, Dh), generator=gg).bfloat16()
+    cache = last.Cache(kp.cuda(), vp.cuda())
+    pages = last.Pages(lens_h=np.asarray([40, 100, 0]), table=torch.from_numpy(table).cuda(),
+                       lens=torch.tensor([70, 112, 1], dtype=torch.int32, device="cuda"))
+    got = last.decode_attention(cache, pages, q.cuda()).cpu().double()
+    out, _, bound, _ = ref.decode(q, kp[0], vp[0], table, (70, 100, 1))
+    assert bool(((got - out).abs() <= bound).all())
+    k, v = (torch.randn((1, 3, Hkv, Dh), generator=gg).bfloat16() for _ in "kv")
+    last.rotary_append(None, cache, pages, None, None, k.cuda(), v.cuda())
+    for pool, x, now in ((kp, k, cache.k), (vp, v, cache.v)):
+        pool[0, 4, :, 5], pool[0, 14, :, 0] = x[0, 0], x[0, 2]      # tokens 69 and 0; 111 lies behind the longest bound
+        assert torch.equal(now.cpu().view(torch.int16), pool.view(torch.int16))
