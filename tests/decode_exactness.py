@@ -55,3 +55,23 @@ def with_parts(q, k, v, parts):
         kept += rest.bfloat16().double()
         rest = p - kept
     return ((kept[..., None] * v.double()).sum(2) / p.sum(-1)[..., None]).bfloat16().double()
+
+
+def repeated(seed, H, Dh, times, dtype):
+    """q [1][H][Dh], k and v [1][H][4 times][Dh]: three cancelling tokens and one whose values are 0, over and over.
+    Four tokens are a part of every tile, so what is left to cancel outside a tile is a rounding's size."""
+    q, k, v = cancelling(seed, 1, H, Dh)
+    zero = torch.zeros(1, H, 1, Dh)
+    return q.to(dtype), torch.cat([k.float(), zero], 2).repeat(1, 1, times, 1).to(dtype), torch.cat([v.float(), zero], 2).repeat(1, 1, times, 1).to(dtype)
+
+
+def exact_repeated(q, k, v):
+    """As `exact`: 4 u T of the probabilities. A tile of n_t keys is added in n_t (fp32) or 3 n_t (bf16, three parts
+    a probability) operations, within a step (2 u) each of what one tile can sum to, its share of T, and the
+    tiles' shares add up to T: 2 u n_t T with n_t = 16, 2 u 96 T with 32. Joining waves and parts adds up residues:
+    under 2 u T, as does each rescaling's rounding, of which there is none after the largest logit, in the first tile."""
+    p = logits(q, k).exp()
+    p = (p / p.sum(-1, keepdim=True))[..., None]
+    out, T = (p * v.double()).sum(2), (p * v.double().abs()).sum(2)
+    u, half, ops = (2.0 ** -24, 2.0 ** -8, 96) if q.dtype == torch.bfloat16 else (2.0 ** -24, 2.0 ** -24, 16)
+    return out, (4 + 2 * ops + 4) * u * T + (half + 16 * u) * out.abs()
