@@ -397,7 +397,9 @@ typedef struct last_cache {
  *   table      [R][max_pages] device: token t of sequence r lies in page
  *              table[r][t / page_size], the same page in every layer. Entries
  *              behind the last page of lens[r] tokens are never read.
- *   table_h    host copy, or NULL where the call allows it
+ *   table_h    host copy, or NULL where the call allows it; where it is given,
+ *              the entries of lens_h[r] tokens must name pages of the cache
+ *              (LAST_ERR_INVALID)
  *   lens       [R] device: tokens of each sequence, 0 allowed
  *   lens_h     [R] host: what lens holds, or (calls that say so) a bound of it
  * The page table and the lengths may change between the replays of a captured
@@ -420,7 +422,7 @@ typedef struct last_pages {
  * for the pairs (x, y) = elements (i, i + n_freqs) of a head, or (2i, 2i + 1)
  * with adjacent != 0. Elements from 2 n_freqs on pass unchanged. inverse != 0
  * turns by -a_i: the inverse, which is also the gradient (the rotation is
- * orthogonal: dx = R^T dy).
+ * orthogonal: dx = R^T dy), a call of its own.
  *   inv_freq   [n_freqs] device fp32, taken as they are: the angle is their
  *              product with the position in 64 bits
  *   axis       [n_freqs] device, and axis_h its host copy: each in [0, n_axes)

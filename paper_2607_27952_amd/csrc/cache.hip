@@ -22,8 +22,8 @@ constexpr int kRowsPrune = 32;   // most new tokens of a block
 constexpr int kItems = 4;        // 16-byte pieces of a thread
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
-// Piece i of a tile of `inner` x `outer` rows of `1 << lc` pieces, as its
-// offset in 16-byte pieces; inner rows are inner_stride pieces apart.
+// Piece i of a tile of rows of `1 << lc` 16-byte pieces, `inner` of them beside
+// each other: its place in its row, and the row's two indices.
 struct Cell {
   int c, inner, outer;
 };

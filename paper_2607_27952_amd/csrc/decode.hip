@@ -2,10 +2,11 @@
 //
 //   s_j = sigma q . k_j,  out = sum_j e^(s_j - m) v_j / sum_j e^(s_j - m)
 //
-// Bound: every cached key and value is read once and used for the Hq / Hkv
-// query heads that share it, a few operations a byte, so the memory bounds it.
-// All that matters is that enough 16-byte loads are in flight; the matrix
-// cores do the products because they make them nearly free.
+// Bound: every cached key and value is read once for each 16 of the Hq / Hkv
+// query heads that share it (17 to 32 read the cache twice), a few operations a
+// byte, so the memory bounds it. All that matters is that enough 16-byte loads
+// are in flight (a lane's share of a bf16 value row of 64 is 8 bytes); the
+// matrix cores do the products because they make them nearly free.
 // 64 sequences of 640 tokens with 32 + 32 heads of 128, 671 MB, take 104 us
 // (6.4 TB/s; sums of rows by the framework that holds the tensors read 6.1).
 //
@@ -545,9 +546,10 @@ namespace last {
 // split 23 us, not split 116 (what this costs is the 5 of the second line);
 // 256 slots with bounds of 0 but for one of 20000, 12 on 2 heads: 16 and 261.
 //
-// A split call has two blocks a compute unit, what its registers let live
-// there: with one the ragged 200 take 57 us for 44, with four the 8 of 16512
-// take 58 for 54.
+// A split call has two blocks a compute unit, what its 212 to 220 registers let
+// live there with heads of 128: with one the ragged 200 take 57 us for 44, with
+// four the 8 of 16512 take 58 for 54. Heads of 64 take 136 to 152, of which three
+// blocks would fit; they have two all the same.
 //
 // Keys of two KV heads beside each other in memory go to one block: 8 of 16512
 // 54 us against 57, 64 of 640 107 against 118 where the heads of a token lie

@@ -666,7 +666,8 @@ def _positions(pos: torch.Tensor, rot: Rotary, T: int, dev: int) -> int:
 
 def rotary(rot: Rotary, pos: torch.Tensor, q: Optional[torch.Tensor], k: Optional[torch.Tensor] = None, q_out=None,
            k_out=None, inverse=False, stream=None):
-    """last_rotary: q and k [G][T][heads][Dh] turned by pos [n_axes][T] (or [T]); inverse is the gradient.
+    """last_rotary: q and k [G][T][heads][Dh] turned by pos [n_axes][T] (or [T]); inverse is the gradient, which
+    the caller asks for: nothing is recorded for autograd, also where q or k requires a gradient.
     Returns (q_out, k_out), None for what is not given; q_out may be q and k_out k."""
     x = q if q is not None else k
     if x is None or x.dim() != 4:
